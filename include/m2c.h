@@ -466,6 +466,167 @@ m2c_status m2c_ratio_search(m2c_layer* layer, const uint16_t* x, int32_t T, int3
                             int32_t* n_high, int32_t* n_low, double* uq, int32_t* count,
                             int32_t* best, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention next to the sparse FFN: whole prompts, and single tokens over a
+ * key/value cache held in 8 bits
+ * ------------------------------------------------------------------------
+ * These calls keep no state in the library: every buffer is the caller's, and
+ * a call only enqueues kernels (m2c_kv_status excepted). Nothing allocates, so
+ * all of them may be captured into a HIP graph.
+ *
+ * Head layout: n_heads query heads over n_kv_heads key/value heads, n_heads a
+ * multiple of n_kv_heads; with G = n_heads / n_kv_heads query head h reads
+ * key/value head h / G. Rows of queries, keys, values and outputs are given by
+ * two strides in elements, between tokens and between heads; the head_dim
+ * elements of a head are contiguous, and pointers and strides are multiples of
+ * 16 bytes (8 elements).
+ *
+ * Softmax statistics and sums are fp32; weights of the value product are
+ * rounded to the 16-bit type of the matrix instruction that takes them. A
+ * masked key contributes nothing, whatever its key and value hold. A query
+ * without any key has a zero output and the log-sum-exp -infinity. */
+enum { M2C_DTYPE_FP16 = 0, M2C_DTYPE_BF16 = 1 };
+
+typedef struct {
+  int32_t dtype;         /* M2C_DTYPE_* of q, k, v and out                      */
+  int32_t n_heads;       /* query heads, 1..1024                                */
+  int32_t n_kv_heads;    /* divides n_heads                                     */
+  int32_t head_dim;      /* 64 or 128                                           */
+  int32_t causal;        /* 1: query i of a sequence with lq queries and lk keys
+                            sees its keys 0 .. lk - lq + i (the last query sees
+                            them all); 0: every key of its sequence             */
+  int32_t device;        /* HIP device ordinal of every pointer                 */
+  float scale;           /* factor of <q, k>; 0 = 1 / sqrt(head_dim)            */
+  int32_t max_q;         /* longest query sequence, or 0 if not known: only
+                            chooses the kernel's tile, never what is computed   */
+  int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2]; /* token, head  */
+} m2c_attn_desc;
+
+/* Attention of packed sequences: rows cu_q[b] .. cu_q[b + 1] - 1 of q and out
+ * and rows cu_k[b] .. cu_k[b + 1] - 1 of k and v are sequence b.
+ *   cu_q, cu_k  dev int32 [n_seqs + 1], ascending, within [0, total_q] and
+ *               [0, total_k]; they may be the same array
+ *   q, out      dev [total_q] rows;  k, v  dev [total_k] rows
+ *   lse         dev fp32 [total_q][n_heads], ln sum exp(scale <q, k>), or NULL
+ * Output rows of no sequence are not written. Results are the same bits on
+ * every run. */
+m2c_status m2c_prompt_attention(const m2c_attn_desc* desc, const void* q, const void* k,
+                                const void* v, const int32_t* cu_q, const int32_t* cu_k,
+                                int32_t n_seqs, int64_t total_q, int64_t total_k, void* out,
+                                float* lse, void* stream);
+
+/* Key/value cache. The tokens of a sequence are cut into blocks of
+ * block_tokens. A block of one key/value head lies in a page:
+ *     amax = max |x| over the block (its keys, and apart its values),
+ *     s    = fp32(amax) / 127                        (IEEE fp32 division),
+ *     code = clamp( rne( fp32(x) / s ), -127, 127 ), 0 if s == 0,
+ *     it stands for code * s.
+ * A block that holds an infinity or a NaN has a scale that is not finite and
+ * codes 0: it reads back as NaN.
+ * The last block of a sequence (the one that holds token len - 1) also keeps
+ * its tokens in their 16-bit type in tail_k / tail_v; they are attended from
+ * there until the block is full, and quantized once, when it is. So what the
+ * cache holds depends on the tokens alone, not on how many came per call.
+ * Every array is the caller's, contiguous device memory of one device: */
+typedef struct {
+  int32_t dtype;         /* M2C_DTYPE_* of the tokens and tails                 */
+  int32_t n_seqs;        /* sequences, 1..65535                                 */
+  int32_t n_kv_heads;    /* 1..1024                                             */
+  int32_t head_dim;      /* 64 or 128                                           */
+  int32_t block_tokens;  /* 32, 64 or 128                                       */
+  int32_t max_blocks;    /* blocks of a sequence, 1..16384                      */
+  int32_t device;
+  int32_t reserved;      /* 0                                                   */
+  int64_t n_pages;       /* pages, 1..2^31 - 1                                  */
+  int8_t* k_codes;       /* [n_pages][block_tokens][head_dim]                   */
+  int8_t* v_codes;
+  float* k_scale;        /* [n_pages]                                           */
+  float* v_scale;
+  void* tail_k;          /* [n_seqs][n_kv_heads][block_tokens][head_dim]        */
+  void* tail_v;
+  int32_t* table;        /* [n_seqs][n_kv_heads][max_blocks] page of each block;
+                            set by the caller for every block that may fill.
+                            Pages that no append fills may be shared            */
+  int32_t* len;          /* [n_seqs] tokens held                                */
+  float* weight;         /* [n_seqs][n_kv_heads][max_blocks] accumulated
+                            attention weight of each block                      */
+  int32_t* arrive;       /* [n_seqs] zeroed once by the caller; library's own   */
+  int32_t* status;       /* [1] zeroed once by the caller; see m2c_kv_status    */
+} m2c_kv_cache;
+
+/* seqs (in the calls below): dev int32 [n], the sequence of each row of the
+ * call, no sequence twice; NULL means sequences 0 .. n - 1. A call that finds
+ * an error on the device leaves that sequence as it was (attend and read give
+ * zero rows) and sets a bit that m2c_kv_status reports. */
+
+/* Forget the tokens of n sequences. */
+m2c_status m2c_kv_reset(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream);
+
+/* Append tokens. Sequence seqs[b] gets rows cu[b] .. cu[b + 1] - 1 of k and v
+ * (cu dev int32 [n + 1], ascending, within [0, total]); cu NULL: row b, one
+ * token each (total == n).
+ *   pos       dev int32 [n], the place of the first new token, or NULL: at the
+ *             end. A place before the end writes over the tokens from there on
+ *             and ends the sequence after the new ones; it must be the start
+ *             of a block or lie in the last block (M2C_ERR_STATE otherwise)
+ *   k_stride, v_stride  token and head strides in elements
+ * The weight of every block that gets its first token is set to 0. A sequence
+ * that would pass max_blocks * block_tokens tokens is M2C_ERR_CAPACITY. */
+m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
+                         const int32_t* cu, int64_t total, const int32_t* pos, const void* k,
+                         const void* v, const int64_t k_stride[2], const int64_t v_stride[2],
+                         void* stream);
+
+/* Read tokens back in the cache's 16-bit type (code * s rounded once; tokens
+ * of the open block as they came): rows cu[b] .. cu[b + 1] - 1 of k and v get
+ * tokens 0, 1, .. of sequence seqs[b], as many as there are; rows past its
+ * length are not written. cu dev int32 [n + 1], ascending, within [0, total]. */
+m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
+                       const int32_t* cu, int64_t total, void* k, void* v,
+                       const int64_t k_stride[2], const int64_t v_stride[2], void* stream);
+
+/* Bytes of the workspace of m2c_kv_attend with the same arguments, or -1. */
+int64_t m2c_kv_attend_workspace(const m2c_kv_cache* cache, int32_t n, int32_t n_heads,
+                                int32_t track, int32_t max_len);
+
+/* Attention of one query token per sequence over everything its sequence
+ * holds.
+ *   q, out     dev [n] rows of n_heads heads, with their strides
+ *   scale      factor of <q, k>; 0 = 1 / sqrt(head_dim)
+ *   lse        dev fp32 [n][n_heads] or NULL
+ *   track      1: adds to weight[s][h][block] the attention weights of the
+ *              block's tokens, summed over the tokens and the query heads of h
+ *   max_len    longest sequence of the call, or 0 if not known (the capacity):
+ *              how far a sequence is split; a longer one is still computed
+ *   workspace  dev, m2c_kv_attend_workspace bytes, 256-byte aligned; not shared
+ *              with a call that may run at the same time
+ * Results are the same bits on every run with the same max_len and n. */
+m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
+                         int32_t n_heads, float scale, const void* q, const int64_t q_stride[2],
+                         void* out, const int64_t out_stride[2], float* lse, int32_t track,
+                         int32_t max_len, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Evict blocks by accumulated weight. The last block of a sequence always
+ * stays; of the m blocks before it every key/value head keeps
+ * `keep` if m > keep (all of them otherwise): the first `first`, the last
+ * `recent`, and of the others the heaviest, ties to the lowest index (weights
+ * compare as the keys of m2c_predict_rank's scores). The entries of the head's
+ * table and weight rows move together: kept blocks in order, then the last
+ * block and the unused entries in order, then the evicted blocks in order with
+ * weight 0 (their pages are the next to be used, or the caller's to take). The
+ * length falls by block_tokens per evicted block.
+ * 0 <= first, 0 <= recent, first + recent <= keep.
+ * table_out, weight_out, len_out: arrays like the cache's that get the rows of
+ * the listed sequences instead, the cache unchanged; all three or none (NULL). */
+m2c_status m2c_kv_evict(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, int32_t keep,
+                        int32_t first, int32_t recent, int32_t* table_out, float* weight_out,
+                        int32_t* len_out, void* stream);
+
+/* Waits for `stream`, then reports and clears what the calls above found on
+ * the device since the last check: M2C_ERR_INVALID_ARG (a sequence or page out
+ * of range), M2C_ERR_CAPACITY, M2C_ERR_STATE, or M2C_OK. */
+m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream);
+
 /* Test support. Copies one record of the host store (no device work). */
 m2c_status m2c_debug_read_record(const m2c_layer* layer, int32_t tier, int32_t neuron, void* out,
                                  size_t bytes);

@@ -1,0 +1,240 @@
+"""Attention of a decoder layer next to the sparse FFN, on torch tensors.
+
+`prompt_attention` attends over whole packed prompts; `KVCache` holds keys and
+values in 8 bits, block by block (`append`, `read`), attends single tokens over
+them (`attend`) and drops the blocks of least accumulated weight (`evict`). The
+work is done by libm2c.so (include/m2c.h has the definitions); this module
+checks tensors and passes addresses.
+
+Every call only enqueues on `stream` (default: torch's current stream) and
+returns. Tensors of a call must stay alive, and not be written elsewhere, until
+its work is done; for outputs that a call allocates torch's allocator sees to
+that on the stream of the call.
+"""
+from __future__ import annotations
+
+import contextlib
+
+import torch
+
+from . import m2c
+
+_DTYPES = {torch.float16: m2c.DTYPE_FP16, torch.bfloat16: m2c.DTYPE_BF16}
+
+
+def _on_stream(stream, device):
+    """Context in which torch allocates for `stream`."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    return torch.cuda.stream(stream)
+
+
+def _bad(msg):
+    raise m2c.M2CError(m2c.M2C_ERR_INVALID_ARG, msg)
+
+
+def _rows(name, t, dtype, device, heads, dim):
+    """Strides (tokens, heads) of rows [tokens][heads][dim]."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        _bad(f"{name}: shape {tuple(t.shape)}, need [tokens, {heads}, {dim}]")
+    if t.dtype != dtype or t.device != device:
+        _bad(f"{name}: {t.dtype} on {t.device}, need {dtype} on {device}")
+    a, b, c = t.stride()
+    if c != 1:
+        _bad(f"{name}: the elements of a head must be contiguous")
+    return (a if t.shape[0] > 1 else 0, b if heads > 1 else 0)
+
+
+def _ints(name, t, n, device):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or t.device != device or \
+            not t.is_contiguous():
+        _bad(f"{name}: need a contiguous int32 tensor of {n} on {device}")
+    return t
+
+
+def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None, out=None,
+                     return_lse=False, stream=None):
+    """Attention of packed prompts.
+
+    q [total_q, n_heads, head_dim]; k, v [total_k, n_kv_heads, head_dim], fp16 or
+    bf16, any token and head strides that are multiples of 8 elements (rows of
+    a fused projection, for example). cu_q, cu_k: int32 [sequences + 1] row
+    starts (cu_k None: the same). causal: query i of lq sees keys 0 .. lk - lq
+    + i of its sequence. max_q: longest query sequence if known (a hint).
+    Returns out like q (contiguous unless given), or (out, lse) with lse fp32
+    [total_q, n_heads] = ln sum exp(scale q.k)."""
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
+        _bad("q, k, v: need fp16 or bf16 GPU tensors [tokens, heads, head_dim]")
+    dev, (tq, hq, d), hk = q.device, q.shape, k.shape[1]
+    desc = m2c.AttnDesc(_DTYPES[q.dtype], hq, hk, d, 1 if causal else 0, dev.index,
+                        0.0 if scale is None else scale, max_q)
+    if v.shape != k.shape:
+        _bad(f"v: shape {tuple(v.shape)}, k has {tuple(k.shape)}")
+    desc.q_stride = _rows("q", q, q.dtype, dev, hq, d)
+    desc.k_stride = _rows("k", k, q.dtype, dev, hk, d)
+    desc.v_stride = _rows("v", v, q.dtype, dev, hk, d)
+    n = cu_q.shape[0] - 1 if cu_q.dim() == 1 else 0
+    if n < 1:
+        _bad("cu_q: need the row starts of at least one sequence and the end")
+    _ints("cu_q", cu_q, n + 1, dev)
+    cu_k = cu_q if cu_k is None else _ints("cu_k", cu_k, n + 1, dev)
+    lse = None
+    if out is None or return_lse:
+        with _on_stream(stream, dev):
+            if out is None:
+                out = torch.empty((tq, hq, d), dtype=q.dtype, device=dev)
+            if return_lse:
+                lse = torch.empty((tq, hq), dtype=torch.float32, device=dev)
+    if out.shape != q.shape:
+        _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+    desc.out_stride = _rows("out", out, q.dtype, dev, hq, d)
+    m2c.m2c_prompt_attention(desc, q, k, v, cu_q, cu_k, n, tq, k.shape[0], out, lse, stream)
+    return (out, lse) if return_lse else out
+
+
+class KVCache:
+    """Keys and values of `n_seqs` sequences in 8 bits, one fp32 scale per
+    block of `block_tokens` tokens of a key/value head.
+
+    Owns (or takes over, with `tensors` naming all but the last two) the arrays
+    of m2c_kv_cache as attributes of the same names: k_codes, v_codes, k_scale,
+    v_scale, tail_k, tail_v, table, len, weight, arrive, status. `n_pages`
+    defaults to one page for every table entry, and `table` to those in order;
+    with fewer pages the caller sets table entries before blocks fill."""
+
+    def __init__(self, n_seqs, n_kv_heads, head_dim, max_blocks, block_tokens=64,
+                 dtype=torch.float16, n_pages=None, device=None, tensors=None):
+        if dtype not in _DTYPES:
+            _bad(f"dtype {dtype}: need torch.float16 or torch.bfloat16")
+        if tensors is not None:
+            dev = tensors["k_codes"].device
+            n_pages = tensors["k_codes"].shape[0]
+        else:
+            dev = torch.device("cuda", torch.cuda.current_device()) if device is None \
+                else torch.device(device)
+            if dev.index is None:
+                dev = torch.device("cuda", torch.cuda.current_device())
+        entries = n_seqs * n_kv_heads * max_blocks
+        n_pages = entries if n_pages is None else n_pages
+        page, tail = (n_pages, block_tokens, head_dim), (n_seqs, n_kv_heads, block_tokens, head_dim)
+        entry = (n_seqs, n_kv_heads, max_blocks)
+        want = {"k_codes": (page, torch.int8), "v_codes": (page, torch.int8),
+                "k_scale": ((n_pages,), torch.float32), "v_scale": ((n_pages,), torch.float32),
+                "tail_k": (tail, dtype), "tail_v": (tail, dtype), "table": (entry, torch.int32),
+                "len": ((n_seqs,), torch.int32), "weight": (entry, torch.float32),
+                "arrive": ((n_seqs,), torch.int32), "status": ((1,), torch.int32)}
+        for name, (shape, dt) in want.items():
+            t = tensors.get(name) if tensors is not None else None
+            if t is None and (tensors is None or name in ("arrive", "status")):
+                make = torch.empty if name in ("k_codes", "v_codes", "tail_k", "tail_v") else torch.zeros
+                t = make(shape, dtype=dt, device=dev)
+                if name == "table":
+                    t = torch.arange(entries, dtype=torch.int32, device=dev).remainder_(n_pages).view(shape)
+            if t is None or tuple(t.shape) != shape or t.dtype != dt or t.device != dev or \
+                    not t.is_contiguous():
+                _bad(f"{name}: need a contiguous {dt} tensor {shape} on {dev}")
+            setattr(self, name, t)
+        self.device, self.dtype = dev, dtype
+        self.n_seqs, self.n_kv_heads, self.head_dim = n_seqs, n_kv_heads, head_dim
+        self.max_blocks, self.block_tokens = max_blocks, block_tokens
+        self.desc = m2c.KvCacheDesc(_DTYPES[dtype], n_seqs, n_kv_heads, head_dim, block_tokens,
+                                    max_blocks, dev.index, 0, n_pages,
+                                    *(getattr(self, n).data_ptr() for n in want))
+
+    def _n(self, seqs, n):
+        """Rows of a call, and its checked sequence list."""
+        if seqs is None:
+            return n, None
+        return seqs.shape[0], _ints("seqs", seqs, n, self.device)
+
+    def reset(self, seqs=None, stream=None):
+        """Forget the tokens of the listed sequences (default: all)."""
+        n = self.n_seqs if seqs is None else seqs.shape[0]
+        n, seqs = self._n(seqs, n)
+        m2c.m2c_kv_reset(self.desc, seqs, n, stream)
+
+    def append(self, k, v, cu=None, seqs=None, pos=None, stream=None):
+        """Append rows of k and v [tokens, n_kv_heads, head_dim]: rows cu[b] ..
+        cu[b + 1] - 1 to sequence seqs[b] (default: b), or with cu None one row
+        each. pos: int32 places of the first new tokens (default: the ends)."""
+        n = k.shape[0] if cu is None else cu.shape[0] - 1
+        n, seqs = self._n(seqs, n)
+        _ints("cu", cu, n + 1, self.device)
+        _ints("pos", pos, n, self.device)
+        ks = _rows("k", k, self.dtype, self.device, self.n_kv_heads, self.head_dim)
+        vs = _rows("v", v, self.dtype, self.device, self.n_kv_heads, self.head_dim)
+        if v.shape[0] != k.shape[0]:
+            _bad(f"v: {v.shape[0]} tokens, k has {k.shape[0]}")
+        m2c.m2c_kv_append(self.desc, seqs, n, cu, k.shape[0], pos, k, v, ks, vs, stream)
+
+    def read(self, cu, total=None, seqs=None, k=None, v=None, stream=None):
+        """Tokens 0, 1, .. of sequence seqs[b] into rows cu[b] .. cu[b + 1] - 1
+        of k and v (allocated with `total` rows if not given; rows past a
+        sequence's length are not written). Returns (k, v)."""
+        n, seqs = self._n(seqs, cu.shape[0] - 1)
+        _ints("cu", cu, n + 1, self.device)
+        if (k is None) != (v is None) or (k is None) == (total is None):
+            _bad("read: give k and v, or total")
+        if k is None:
+            with _on_stream(stream, self.device):
+                k, v = (torch.empty((total, self.n_kv_heads, self.head_dim), dtype=self.dtype,
+                                    device=self.device) for _ in range(2))
+        ks = _rows("k", k, self.dtype, self.device, self.n_kv_heads, self.head_dim)
+        vs = _rows("v", v, self.dtype, self.device, self.n_kv_heads, self.head_dim)
+        if v.shape[0] != k.shape[0]:
+            _bad(f"v: {v.shape[0]} rows, k has {k.shape[0]}")
+        m2c.m2c_kv_read(self.desc, seqs, n, cu, k.shape[0], k, v, ks, vs, stream)
+        return k, v
+
+    def attend(self, q, seqs=None, max_len=0, scale=None, track=False, out=None, return_lse=False,
+               stream=None):
+        """Attention of one token per sequence, q [n, n_heads, head_dim], over
+        all that sequence seqs[b] (default: b) holds. max_len: the longest of
+        them if known. track: add the blocks' attention weights to `weight`.
+        Returns out like q, or (out, lse) with lse fp32 [n, n_heads]."""
+        if q.dim() != 3:
+            _bad("q: need [n, n_heads, head_dim]")
+        hq = q.shape[1]
+        n, seqs = self._n(seqs, q.shape[0])
+        qs = _rows("q", q, self.dtype, self.device, hq, self.head_dim)
+        track = 1 if track else 0
+        need = m2c.m2c_kv_attend_workspace(self.desc, n, hq, track, max_len)
+        lse = work = None
+        with _on_stream(stream, self.device):
+            if out is None:
+                out = torch.empty((n, hq, self.head_dim), dtype=self.dtype, device=self.device)
+            if return_lse:
+                lse = torch.empty((n, hq), dtype=torch.float32, device=self.device)
+            if need:
+                work = torch.empty(need, dtype=torch.uint8, device=self.device)
+        if out.shape != q.shape:
+            _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+        os = _rows("out", out, self.dtype, self.device, hq, self.head_dim)
+        m2c.m2c_kv_attend(self.desc, seqs, n, hq, 0.0 if scale is None else scale, q, qs, out, os,
+                          lse, track, max_len, work, need, stream)
+        return (out, lse) if return_lse else out
+
+    def evict(self, keep, first=0, recent=0, seqs=None, out=None, stream=None):
+        """Keep `keep` blocks before the last one of every listed sequence and
+        head: the first `first`, the last `recent`, else the heaviest. out: a
+        dict of tensors "table", "weight", "len" that get the rows instead of
+        the cache's own."""
+        n, seqs = self._n(seqs, self.n_seqs if seqs is None else seqs.shape[0])
+        to = (None, None, None)
+        if out is not None:
+            to = tuple(out[name] for name in ("table", "weight", "len"))
+            for name, t in zip(("table", "weight", "len"), to):
+                own = getattr(self, name)
+                if t.shape != own.shape or t.dtype != own.dtype or t.device != own.device or \
+                        not t.is_contiguous():
+                    _bad(f"out[{name!r}]: need a tensor like the cache's")
+        m2c.m2c_kv_evict(self.desc, seqs, n, keep, first, recent, *to, stream)
+
+    def check(self, stream=None):
+        """Wait for `stream`; raise what the calls so far found on the device
+        (a sequence or page out of range, a full sequence, a bad place)."""
+        m2c.m2c_kv_status(self.desc, stream)

@@ -1,0 +1,533 @@
+// Attention of one query token per sequence over the 8-bit key/value cache.
+//
+// Per query head over the tokens the sequence holds, in units of 2^: with
+// c = scale * log2 e, x_t = c <q, code_t> s_k (s_k the block's key scale),
+//   m = max x_t, p_t = 2^(x_t - m), l = sum p_t, O = sum_blocks s_v sum p_t code_t / l.
+// Every code byte is read once, by one wave, for all query heads of its
+// key/value head: bound by the bytes of the pages.
+//
+// Transposed products on 16x16x32 instructions: S^T = K Q^T (rows tokens,
+// columns the up to 16 query heads of the group), O^T = V^T P^T. A lane's
+// column is one query head, the softmax runs down registers and across the
+// four lanes of a column, and S^T's registers, rounded in pairs, are the second
+// product's B operand as they lie: a lane of quarter c = l / 16 holds tokens
+// {4c .. 4c + 3, 16 + 4c .. 16 + 4c + 3} of each 32, and V's rows are loaded in
+// that order. Codes become fp16 exactly; queries of bf16 caches are scaled by a
+// power of two per head into fp16's range (exact but for elements 2^-24 of the
+// head's largest). So both products sum exact products in fp32, p alone is
+// rounded (fp16, relative 2^-12).
+//
+// A sequence is split into chunks of units; each workgroup's four waves take a
+// chunk's units in turn, each with its own running m, l, O, joined through LDS;
+// chunks are joined by a second launch where there are several.
+#include "ffn_device.h"
+#include "kv_device.h"
+
+namespace m2c {
+
+struct AttendArgs {
+  KvView C;
+  const int32_t* seqs;
+  const uint8_t* q;
+  uint8_t* out;
+  float* lse;
+  int64_t q_row, q_head, o_row, o_head;  // bytes
+  float* part_o;    // [n][n_heads][splits][D] unnormalized outputs of the splits
+  float2* part_ml;  // [n][n_heads][splits] their m and l
+  float2* fin;      // [n][n_heads] m and 1 / l of the whole (track)
+  float2* wsum;     // [n][n_kv_heads][units of max_blocks][group] m and sum of p by unit (track)
+  float c;
+  int n, n_heads, group, tiles;  // tiles: head tiles of 16 per key/value head
+  int splits, chunk;             // chunk: units per workgroup
+};
+
+namespace {
+
+constexpr int kWaves = 4;
+
+// p of a unit's tokens from its scores, and the running statistics. s: scores
+// in units of 2^ (masked ones -infinity). Returns the factor for what was
+// summed before; *unit_sum the lane's sum of p.
+template <int T>
+__device__ __forceinline__ float softmax_step(f32x4 (&s)[T], float& m, float& l, float* unit_sum) {
+  float mt = s[0][0];
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mt = fmaxf(mt, s[t][r]);
+  mt = max_xor16(max_xor32(mt));
+  const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
+  const float alpha = exp2_fast(m - mu);
+  m = mn;
+  const float base = mu - kLift;
+  float sum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < T; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[t][r] = exp2_fast(s[t][r] - base);
+      sum += s[t][r];
+    }
+  l = l * alpha + sum;
+  *unit_sum = sum;
+  return alpha;
+}
+
+// 32 tokens' p as the B operand of the value product.
+template <bool BF>
+__device__ __forceinline__ u32x4 pack_p(const f32x4& a, const f32x4& b) {
+  return u32x4{pack16<BF>(a[0], a[1]), pack16<BF>(a[2], a[3]), pack16<BF>(b[0], b[1]),
+               pack16<BF>(b[2], b[3])};
+}
+
+// Byte i of two rows' words as a pair of fp16 (offset-binary codes, see
+// i8x4_to_h2).
+template <int I>
+__device__ __forceinline__ uint32_t pair_of(uint32_t lo, uint32_t hi) {
+  constexpr uint32_t sel = 0x0c000c00u | (uint32_t)I | (uint32_t)(4 + I) << 16;
+  const uint32_t u = __builtin_amdgcn_perm(hi, lo, sel) | 0x64006400u;
+  const half2v bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+  return __builtin_bit_cast(uint32_t, (half2v)(as_h2(u) - bias));
+}
+
+template <bool BF, int D, int UNIT>
+__global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs A) {
+  constexpr int T = UNIT / 16;   // token tiles of a unit
+  constexpr int KS = D / 32;     // steps of the score product
+  constexpr int KL = D / 64;     // 16-byte loads of a key row per lane
+  constexpr int E = D / 16;      // dimensions of a lane in the value product
+  constexpr int VW = E / 4;      // code words of those
+  constexpr int V2 = UNIT / 32;  // steps of the value product
+  __shared__ __align__(16) float mrg[kWaves][16][D + 4];
+  __shared__ float2 mls[kWaves][16];
+
+  const KvView& C = A.C;
+  const int lane = threadIdx.x & 63, col = lane & 15, qr = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.x / A.splits, split = blockIdx.x - row * A.splits;
+  const int ht = row % A.tiles, rk = row / A.tiles;
+  const int b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
+  const int heads = min(16, A.group - ht * 16);           // query heads of this tile
+  const int h0 = kvh * A.group + ht * 16;                 // the first
+  const int BT = C.block_tokens, per_block = BT / UNIT;
+  const int s_id = A.seqs ? A.seqs[b] : b;
+  const bool known = s_id >= 0 && s_id < C.n_seqs;
+  const int s = known ? s_id : 0;
+  if (!known && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
+  const int len = known ? (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * BT) : 0;
+  const int full = len / BT * per_block;                  // units that lie in pages
+  const int units = full + (len - len / BT * BT + UNIT - 1) / UNIT;
+  const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
+  const int32_t* table = C.table + sh * C.max_blocks;
+  float2* wsum = A.wsum ? A.wsum + ((int64_t)rk * C.max_blocks * per_block) * A.group + ht * 16 + col
+                        : nullptr;
+
+  // queries: column = head, a step's elements where the key loads have them
+  u32x4 qf[KS];
+  const uint8_t* qrow = A.q + b * A.q_row + (h0 + min(col, heads - 1)) * A.q_head;
+#pragma unroll
+  for (int k = 0; k < KS; ++k) qf[k] = *(const u32x4*)(qrow + ((k / 2) * 64 + qr * 16 + (k & 1) * 8) * 2);
+  float qc = A.c;
+  if constexpr (BF) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t u = qf[k][w];
+        const uint32_t a = u & 0x7fffu, d = u >> 16 & 0x7fffu;
+        big = max(big, max(a < 0x7f80u ? a : 0u, d < 0x7f80u ? d : 0u));
+      }
+    big = max(big, (uint32_t)__shfl_xor((int)big, 16));
+    big = max(big, (uint32_t)__shfl_xor((int)big, 32));
+    const int ex = big >= 0x80u ? (int)(big >> 7) - 127 : big ? -126 : 14;  // the largest is below 2^(ex + 1)
+    const int up = 14 - ex;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t u = qf[k][w];
+        qf[k][w] = pack16<false>(ldexpf(unpack16<true>(u & 0xffffu), up), ldexpf(unpack16<true>(u >> 16), up));
+      }
+    qc = ldexpf(A.c, -up);
+  }
+
+  f32x4 o[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, l = 0.0f;
+
+  for (int u0 = split * A.chunk; u0 < units; u0 += A.splits * A.chunk) {
+    const int u1 = min(units, u0 + A.chunk);
+    // A wave's units of the chunk are u0 + wave, + kWaves, .. (at most 64);
+    // lane i holds the page and scales of its i-th.
+    const int mine = u0 + wave + kWaves * lane;
+    int page = 0;
+    float sk = 0.0f, sv = 0.0f;
+    if (mine < min(u1, full)) {
+      page = table[mine / per_block];
+      if (page < 0 || page >= C.n_pages) {
+        atomicOr(C.status, kKvBadIndex);
+        page = 0;  // in bounds; a scale of 0 makes a block of zeros of it
+      } else {
+        sk = C.k_scale[page];
+        sv = C.v_scale[page];
+      }
+    }
+    for (int u = u0 + wave, i = 0; u < min(u1, full); u += kWaves, ++i) {
+      const int pg = __builtin_amdgcn_readlane(page, i);
+      const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sk), i));
+      const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sv), i));
+      const int64_t at = ((int64_t)pg * BT + (u % per_block) * UNIT) * D;
+      const int8_t* kp = C.k_codes + at + col * D + qr * 16;
+      const int8_t* vp = C.v_codes + at + qr * 4 * D + col * E;
+      u32x4 kw[T][KL];
+      uint32_t vw[V2][8][VW];
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int k = 0; k < KL; ++k) kw[t][k] = *(const u32x4*)(kp + t * 16 * D + k * 64);
+#pragma unroll
+      for (int v = 0; v < V2; ++v)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int8_t* p = vp + (v * 32 + (j / 4) * 16 + j % 4) * D;
+          if constexpr (VW == 2) {
+            const u32x2 w = *(const u32x2*)p;
+            vw[v][j][0] = w[0], vw[v][j][1] = w[1];
+          } else {
+            vw[v][j][0] = *(const uint32_t*)p;
+          }
+        }
+      f32x4 x[T];
+      const float f = ks * qc;
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          half2v a, d, e, g;
+          i8x4_to_h2(kw[t][k / 2][(k & 1) * 2], a, d);
+          i8x4_to_h2(kw[t][k / 2][(k & 1) * 2 + 1], e, g);
+          const u32x4 kf = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, d),
+                            __builtin_bit_cast(uint32_t, e), __builtin_bit_cast(uint32_t, g)};
+          x[t] = mfma16<false>(kf, qf[k], x[t]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[t][r] *= f;
+      }
+      float sum;
+      const float alpha = softmax_step<T>(x, m, l, &sum);
+      if (wsum) {
+        sum = add_xor16(add_xor32(sum));
+        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
+      }
+      f32x4 acc[E];
+#pragma unroll
+      for (int i2 = 0; i2 < E; ++i2) acc[i2] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int v = 0; v < V2; ++v) {
+        const u32x4 pf = pack_p<false>(x[2 * v], x[2 * v + 1]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vw[v][j][w] ^= 0x80808080u;
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          auto frag = [&](auto idx) {
+            constexpr int I = decltype(idx)::value;
+            const u32x4 vf = {pair_of<I>(vw[v][0][w], vw[v][1][w]), pair_of<I>(vw[v][2][w], vw[v][3][w]),
+                              pair_of<I>(vw[v][4][w], vw[v][5][w]), pair_of<I>(vw[v][6][w], vw[v][7][w])};
+            acc[w * 4 + I] = mfma16<false>(vf, pf, acc[w * 4 + I]);
+          };
+          frag(std::integral_constant<int, 0>());
+          frag(std::integral_constant<int, 1>());
+          frag(std::integral_constant<int, 2>());
+          frag(std::integral_constant<int, 3>());
+        }
+      }
+#pragma unroll
+      for (int i2 = 0; i2 < E; ++i2)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i2][r] = fmaf(acc[i2][r], vs, o[i2][r] * alpha);
+    }
+    // units of the open block, from the 16-bit tail; rows past the length are
+    // zeros, whatever the tail holds there
+    for (int u = u0 + wave; u < u1; u += kWaves) {
+      if (u < full) continue;
+      const int t_first = u * UNIT - len / BT * BT, left = len % BT - t_first;
+      const uint8_t* kt = C.tail_k + (sh * BT + t_first) * (D * 2);
+      const uint8_t* vt = C.tail_v + (sh * BT + t_first) * (D * 2);
+      f32x4 x[T];
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const bool in = t * 16 + col < left;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const int el = (k / 2) * 64 + qr * 16 + (k & 1) * 8;
+          const u32x4 qw = *(const u32x4*)(qrow + el * 2);
+          const u32x4 kf = in ? *(const u32x4*)(kt + ((t * 16 + col) * D + el) * 2) : u32x4{0, 0, 0, 0};
+          x[t] = mfma16<BF>(kf, qw, x[t]);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          x[t][r] = t * 16 + qr * 4 + r < left ? x[t][r] * A.c : -INFINITY;
+      }
+      float sum;
+      const float alpha = softmax_step<T>(x, m, l, &sum);
+      if (wsum) {
+        sum = add_xor16(add_xor32(sum));
+        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
+#pragma unroll
+      for (int v = 0; v < V2; ++v) {
+        const u32x4 pf = pack_p<BF>(x[2 * v], x[2 * v + 1]);
+        uint32_t w[8][E / 2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int tok = v * 32 + (j / 4) * 16 + qr * 4 + j % 4;
+#pragma unroll
+          for (int e = 0; e < E / 2; ++e) w[j][e] = 0;
+          if (tok < left) {
+            const uint32_t* p = (const uint32_t*)(vt + (tok * D + col * E) * 2);
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) w[j][e] = p[e];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
+          const u32x4 vf = {__builtin_amdgcn_perm(w[1][i / 2], w[0][i / 2], sel),
+                            __builtin_amdgcn_perm(w[3][i / 2], w[2][i / 2], sel),
+                            __builtin_amdgcn_perm(w[5][i / 2], w[4][i / 2], sel),
+                            __builtin_amdgcn_perm(w[7][i / 2], w[6][i / 2], sel)};
+          o[i] = mfma16<BF>(vf, pf, o[i]);
+        }
+      }
+    }
+  }
+
+  // Join the waves. Lane (col, qr) holds dimensions (4 qr + r) E + i of head col.
+  l = add_xor16(add_xor32(l));
+  if (lane < 16) mls[wave][col] = make_float2(m, l);
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int i = 0; i < E; i += 4)
+      *(f32x4*)&mrg[wave][col][(qr * 4 + r) * E + i] = f32x4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]};
+  __syncthreads();
+  const int hd = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * E;
+  if (hd >= heads) return;
+  float M = -INFINITY, L = 0.0f, fac[kWaves];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mls[w][hd].x);
+  const float mu = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    fac[w] = exp2_fast(mls[w][hd].x - mu);
+    L += mls[w][hd].y * fac[w];
+  }
+  float y[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) y[i] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+    for (int i = 0; i < E; ++i) y[i] = fmaf(mrg[w][hd][d0 + i], fac[w], y[i]);
+  const int64_t at = (int64_t)b * A.n_heads + h0 + hd;
+  if (A.splits > 1) {
+    if ((threadIdx.x & 15) == 0) A.part_ml[at * A.splits + split] = make_float2(M, L);
+    float* po = A.part_o + (at * A.splits + split) * D + d0;
+#pragma unroll
+    for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    return;
+  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  uint32_t* po = (uint32_t*)(A.out + b * A.o_row + (h0 + hd) * A.o_head + d0 * 2);
+#pragma unroll
+  for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
+  if ((threadIdx.x & 15) == 0) {
+    if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
+    if (A.fin) A.fin[at] = make_float2(M, inv);
+  }
+}
+
+// Joins the splits of one query head: 256 threads, D / 4 of them per split.
+template <bool BF, int D>
+__global__ void __launch_bounds__(256) join_kernel(const AttendArgs A) {
+  constexpr int TS = D / 4, GR = 256 / TS;
+  __shared__ __align__(16) f32x4 acc[GR][TS];
+  const int tid = threadIdx.x;
+  const int64_t at = blockIdx.x;
+  const float2* ml = A.part_ml + at * A.splits;
+  float M = -INFINITY, L = 0.0f;
+  for (int s = tid & 63; s < A.splits; s += 64) M = fmaxf(M, ml[s].x);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  const float mu = M == -INFINITY ? 0.0f : M;
+  for (int s = tid & 63; s < A.splits; s += 64) L += ml[s].y * exp2_fast(ml[s].x - mu);
+  L = wave_sum(L);
+  f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+  const float* po = A.part_o + at * A.splits * D + (tid % TS) * 4;
+  for (int s = tid / TS; s < A.splits; s += GR) {
+    const float f = exp2_fast(ml[s].x - mu);
+    const f32x4 v = *(const f32x4*)(po + (int64_t)s * D);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], f, y[i]);
+  }
+  acc[tid / TS][tid % TS] = y;
+  __syncthreads();
+  if (tid >= TS) return;
+#pragma unroll
+  for (int g = 1; g < GR; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] += acc[g][tid][i];
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  const int64_t b = at / A.n_heads, h = at - b * A.n_heads;
+  uint32_t* out = (uint32_t*)(A.out + b * A.o_row + h * A.o_head + tid * 8);
+  out[0] = pack16<BF>(y[0] * inv, y[1] * inv);
+  out[1] = pack16<BF>(y[2] * inv, y[3] * inv);
+  if (tid == 0) {
+    if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
+    if (A.fin) A.fin[at] = make_float2(M, inv);
+  }
+}
+
+// weight[s][h][block] += sum over the block's units and the group's heads of
+// (sum of p) 2^(m_unit - m) / l.
+__global__ void __launch_bounds__(256) weigh_kernel(const AttendArgs A, int unit, int parts) {
+  const KvView& C = A.C;
+  const int per_block = C.block_tokens / unit;
+  const int rk = blockIdx.x / parts, part = blockIdx.x - rk * parts, b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
+  const int s = A.seqs ? A.seqs[b] : b;
+  if (s < 0 || s >= C.n_seqs) return;
+  const int len = (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * C.block_tokens);
+  const int units = len / C.block_tokens * per_block + (len % C.block_tokens + unit - 1) / unit;
+  const float2* fin = A.fin + (int64_t)b * A.n_heads + kvh * A.group;
+  for (int blk = part * 256 + threadIdx.x; blk * C.block_tokens < len; blk += parts * 256) {
+    float w = 0.0f;
+    for (int u = blk * per_block; u < min(units, (blk + 1) * per_block); ++u) {
+      const float2* p = A.wsum + ((int64_t)rk * C.max_blocks * per_block + u) * A.group;
+      for (int g = 0; g < A.group; ++g) {
+        const float m = fin[g].x == -INFINITY ? 0.0f : fin[g].x;
+        w += p[g].y * exp2_fast(p[g].x - m) * fin[g].y;
+      }
+    }
+    C.weight[((int64_t)s * C.n_kv_heads + kvh) * C.max_blocks + blk] += w;
+  }
+}
+
+int unit_of(const KvView& C) { return C.block_tokens < 64 ? 32 : 64; }
+
+struct Split {
+  int tiles, splits, chunk;
+};
+
+Split split_of(const KvView& C, int n, int n_heads, int max_len) {
+  const int unit = unit_of(C), group = n_heads / C.n_kv_heads;
+  const int64_t cap = (int64_t)C.max_blocks * C.block_tokens;
+  const int64_t most = max_len > 0 && max_len < cap ? max_len : cap;
+  const int units = (int)((most + unit - 1) / unit);
+  Split S;
+  S.tiles = (group + 15) / 16;
+  const int64_t rows = (int64_t)n * C.n_kv_heads * S.tiles;
+  int64_t chunk = (rows * units + 2047) / 2048;
+  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+  chunk = chunk < 8 ? 8 : chunk > 64 ? 64 : chunk;
+  while ((units + chunk - 1) / chunk > 1024) chunk += kWaves;
+  S.chunk = (int)chunk;
+  S.splits = (int)((units + chunk - 1) / chunk);
+  if (S.splits < 1) S.splits = 1;
+  return S;
+}
+
+int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+int64_t kv_attend_workspace(const KvView& C, int n, int n_heads, int track, int max_len) {
+  const Split S = split_of(C, n, n_heads, max_len);
+  int64_t bytes = 0;
+  if (S.splits > 1)
+    bytes += round256((int64_t)n * n_heads * S.splits * 8) +
+             round256((int64_t)n * n_heads * S.splits * C.head_dim * 4);
+  if (track)
+    bytes += round256((int64_t)n * n_heads * 8) +
+             round256((int64_t)n * n_heads * C.max_blocks * (C.block_tokens / unit_of(C)) * 8);
+  return bytes;
+}
+
+hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_heads, float scale,
+                            const void* q, const int64_t* qs, void* out, const int64_t* os,
+                            float* lse, int track, int max_len, void* workspace, hipStream_t stream) {
+  const Split S = split_of(C, n, n_heads, max_len);
+  AttendArgs A = {};
+  A.C = C;
+  A.seqs = seqs;
+  A.q = (const uint8_t*)q;
+  A.out = (uint8_t*)out;
+  A.lse = lse;
+  A.q_row = qs[0] * 2, A.q_head = qs[1] * 2;
+  A.o_row = os[0] * 2, A.o_head = os[1] * 2;
+  A.c = (scale > 0.0f ? scale : 1.0f / sqrtf((float)C.head_dim)) * kLog2e;
+  A.n = n;
+  A.n_heads = n_heads;
+  A.group = n_heads / C.n_kv_heads;
+  A.tiles = S.tiles;
+  A.splits = S.splits;
+  A.chunk = S.chunk;
+  uint8_t* ws = (uint8_t*)workspace;
+  if (S.splits > 1) {
+    A.part_ml = (float2*)ws;
+    ws += round256((int64_t)n * n_heads * S.splits * 8);
+    A.part_o = (float*)ws;
+    ws += round256((int64_t)n * n_heads * S.splits * C.head_dim * 4);
+  }
+  if (track) {
+    A.fin = (float2*)ws;
+    ws += round256((int64_t)n * n_heads * 8);
+    A.wsum = (float2*)ws;
+  }
+  const int unit = unit_of(C);
+  const int64_t grid = (int64_t)n * C.n_kv_heads * S.tiles * S.splits;
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
+#define M2C_ATTEND(BF, D, U) \
+  hipLaunchKernelGGL((attend_kernel<BF, D, U>), dim3((uint32_t)grid), dim3(kWaves * 64), 0, stream, A)
+#define M2C_JOIN(BF, D) \
+  hipLaunchKernelGGL((join_kernel<BF, D>), dim3((uint32_t)((int64_t)n * n_heads)), dim3(256), 0, stream, A)
+  if (C.head_dim == 128) {
+    if (unit == 64) { if (C.bf) M2C_ATTEND(true, 128, 64); else M2C_ATTEND(false, 128, 64); }
+    else { if (C.bf) M2C_ATTEND(true, 128, 32); else M2C_ATTEND(false, 128, 32); }
+  } else {
+    if (unit == 64) { if (C.bf) M2C_ATTEND(true, 64, 64); else M2C_ATTEND(false, 64, 64); }
+    else { if (C.bf) M2C_ATTEND(true, 64, 32); else M2C_ATTEND(false, 64, 32); }
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (S.splits > 1) {
+    if (C.head_dim == 128) { if (C.bf) M2C_JOIN(true, 128); else M2C_JOIN(false, 128); }
+    else { if (C.bf) M2C_JOIN(true, 64); else M2C_JOIN(false, 64); }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (track) {
+    const int64_t cap = (int64_t)C.max_blocks * C.block_tokens;
+    const int64_t most = max_len > 0 && max_len < cap ? max_len : cap;
+    const int64_t blocks = (most + C.block_tokens - 1) / C.block_tokens;
+    const int parts = (int)((blocks + 255) / 256);
+    if ((int64_t)n * C.n_kv_heads * parts > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(weigh_kernel, dim3((uint32_t)(n * C.n_kv_heads * parts)), dim3(256), 0, stream,
+                       A, unit, parts);
+    e = hipGetLastError();
+  }
+#undef M2C_ATTEND
+#undef M2C_JOIN
+  return e;
+}
+
+}  // namespace m2c

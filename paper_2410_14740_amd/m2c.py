@@ -84,6 +84,25 @@ class DramStats(ctypes.Structure):
                 ("wait_seconds", ctypes.c_double), ("direct_io", ctypes.c_int32)]
 
 
+DTYPE_FP16, DTYPE_BF16 = range(2)
+_I64x2 = ctypes.c_int64 * 2
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "dtype", "n_heads", "n_kv_heads", "head_dim", "causal", "device")] + [
+        ("scale", ctypes.c_float), ("max_q", ctypes.c_int32)] + [
+        (n, _I64x2) for n in ("q_stride", "k_stride", "v_stride", "out_stride")]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "dtype", "n_seqs", "n_kv_heads", "head_dim", "block_tokens", "max_blocks", "device",
+        "reserved")] + [("n_pages", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in (
+            "k_codes", "v_codes", "k_scale", "v_scale", "tail_k", "tail_v", "table", "len",
+            "weight", "arrive", "status")]
+
+
 class Stats(ctypes.Structure):
     _fields_ = [("plans", ctypes.c_int64), ("req", ctypes.c_int64), ("hit", ctypes.c_int64),
                 ("refill", ctypes.c_int64), ("new_", ctypes.c_int64), ("bypass", ctypes.c_int64),
@@ -141,6 +160,17 @@ def load(path: str = LIB_PATH):
                                              ctypes.POINTER(P)]),
         "m2c_ratio_search": (I32, [P, P, I32, I32, I32, I32, I32, P, P, P,
                                    ctypes.POINTER(I32), ctypes.POINTER(I32), P]),
+        "m2c_prompt_attention": (I32, [ctypes.POINTER(AttnDesc), P, P, P, P, P, I32, I64, I64, P, P,
+                                       P]),
+        "m2c_kv_reset": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P]),
+        "m2c_kv_append": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, P, P, P, _I64x2, _I64x2,
+                                P]),
+        "m2c_kv_read": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, P, P, _I64x2, _I64x2, P]),
+        "m2c_kv_attend_workspace": (I64, [ctypes.POINTER(KvCacheDesc), I32, I32, I32, I32]),
+        "m2c_kv_attend": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, ctypes.c_float, P, _I64x2,
+                                P, _I64x2, P, I32, I32, P, I64, P]),
+        "m2c_kv_evict": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, I32, I32, P, P, P, P]),
+        "m2c_kv_status": (I32, [ctypes.POINTER(KvCacheDesc), P]),
         "m2c_last_error": (ctypes.c_char_p, []),
         "m2c_build_id": (ctypes.c_char_p, []),
     }
@@ -387,6 +417,54 @@ def m2c_debug_read_pool_tables(layer, tier: int, d_ff: int, C: int):
     _check(load().m2c_debug_read_pool_tables(layer, tier, slot_of.ctypes.data, key.ctypes.data,
                                              last.ctypes.data))
     return slot_of, key[:C], last[:C]
+
+
+def m2c_prompt_attention(desc: AttnDesc, q, k, v, cu_q, cu_k, n_seqs: int, total_q: int, total_k: int,
+                         out, lse=None, stream=None):
+    _check(load().m2c_prompt_attention(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k),
+                                       n_seqs, total_q, total_k, _ptr(out), _ptr(lse),
+                                       _stream(stream)))
+
+
+def m2c_kv_reset(cache: KvCacheDesc, seqs, n: int, stream=None):
+    _check(load().m2c_kv_reset(cache, _ptr(seqs), n, _stream(stream)))
+
+
+def m2c_kv_append(cache: KvCacheDesc, seqs, n: int, cu, total: int, pos, k, v, k_stride, v_stride,
+                  stream=None):
+    _check(load().m2c_kv_append(cache, _ptr(seqs), n, _ptr(cu), total, _ptr(pos), _ptr(k), _ptr(v),
+                                _I64x2(*k_stride), _I64x2(*v_stride), _stream(stream)))
+
+
+def m2c_kv_read(cache: KvCacheDesc, seqs, n: int, cu, total: int, k, v, k_stride, v_stride,
+                stream=None):
+    _check(load().m2c_kv_read(cache, _ptr(seqs), n, _ptr(cu), total, _ptr(k), _ptr(v),
+                              _I64x2(*k_stride), _I64x2(*v_stride), _stream(stream)))
+
+
+def m2c_kv_attend_workspace(cache: KvCacheDesc, n: int, n_heads: int, track: int, max_len: int) -> int:
+    need = load().m2c_kv_attend_workspace(cache, n, n_heads, track, max_len)
+    if need < 0:
+        raise M2CError(M2C_ERR_INVALID_ARG, load().m2c_last_error().decode())
+    return need
+
+
+def m2c_kv_attend(cache: KvCacheDesc, seqs, n: int, n_heads: int, scale: float, q, q_stride, out,
+                  out_stride, lse, track: int, max_len: int, workspace, workspace_bytes: int,
+                  stream=None):
+    _check(load().m2c_kv_attend(cache, _ptr(seqs), n, n_heads, scale, _ptr(q), _I64x2(*q_stride),
+                                _ptr(out), _I64x2(*out_stride), _ptr(lse), track, max_len,
+                                _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def m2c_kv_evict(cache: KvCacheDesc, seqs, n: int, keep: int, first: int, recent: int,
+                 table_out=None, weight_out=None, len_out=None, stream=None):
+    _check(load().m2c_kv_evict(cache, _ptr(seqs), n, keep, first, recent, _ptr(table_out),
+                               _ptr(weight_out), _ptr(len_out), _stream(stream)))
+
+
+def m2c_kv_status(cache: KvCacheDesc, stream=None):
+    _check(load().m2c_kv_status(cache, _stream(stream)))
 
 
 def m2c_last_error() -> str:
