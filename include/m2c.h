@@ -477,9 +477,9 @@ m2c_status m2c_ratio_search(m2c_layer* layer, const uint16_t* x, int32_t T, int3
  * Head layout: n_heads query heads over n_kv_heads key/value heads, n_heads a
  * multiple of n_kv_heads; with G = n_heads / n_kv_heads query head h reads
  * key/value head h / G. Rows of queries, keys, values and outputs are given by
- * two strides in elements, between tokens and between heads; the head_dim
- * elements of a head are contiguous, and pointers and strides are multiples of
- * 16 bytes (8 elements).
+ * two strides in elements, between tokens (head_dim .. 2^24) and between heads
+ * (0 for keys or values that heads share); the head_dim elements of a head are
+ * contiguous, and pointers and strides are multiples of 16 bytes (8 elements).
  *
  * Softmax statistics and sums are fp32; weights of the value product are
  * rounded to the 16-bit type of the matrix instruction that takes them. A

@@ -44,7 +44,7 @@ def _rows(name, t, dtype, device, heads, dim):
     a, b, c = t.stride()
     if c != 1:
         _bad(f"{name}: the elements of a head must be contiguous")
-    return (a if t.shape[0] > 1 else 0, b if heads > 1 else 0)
+    return (a if t.shape[0] > 1 else dim, b if heads > 1 else 0)  # a single row's stride is free
 
 
 def _ints(name, t, n, device):

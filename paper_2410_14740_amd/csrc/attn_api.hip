@@ -34,15 +34,22 @@ m2c_status launched(hipError_t e, const char* what) {
 
 constexpr int64_t kMaxRows = 1 << 30;  // rows of a call: their indices and those past the last fit 32 bits
 
+constexpr int64_t kMaxTokenStride = 1 << 24;
+
 bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
-m2c_status check_rows(const char* what, const void* p, const int64_t* stride) {
+// Rows may share heads (a head stride of 0), but tokens lie apart; a tile of
+// them spans less than 4 GB.
+m2c_status check_rows(const char* what, const void* p, const int64_t* stride, int head_dim) {
   if (!p || !stride) return api_fail(M2C_ERR_INVALID_ARG, "%s: NULL argument", what);
   if (misaligned(p)) return api_fail(M2C_ERR_INVALID_ARG, "%s: not 16-byte aligned", what);
   for (int i = 0; i < 2; ++i)
     if (stride[i] < 0 || stride[i] % 8 || stride[i] > ((int64_t)1 << 40))
       return api_fail(M2C_ERR_INVALID_ARG, "%s: stride %lld: need a multiple of 8 elements, >= 0",
                       what, (long long)stride[i]);
+  if (stride[0] < head_dim || stride[0] > kMaxTokenStride)
+    return api_fail(M2C_ERR_INVALID_ARG, "%s: token stride %lld: need [head_dim, 2^24] elements", what,
+                    (long long)stride[0]);
   return M2C_OK;
 }
 
@@ -122,11 +129,11 @@ m2c_status m2c_prompt_attention(const m2c_attn_desc* D, const void* q, const voi
     return api_fail(M2C_ERR_INVALID_ARG, "total_q %lld, total_k %lld: need [0, 2^30]",
                     (long long)total_q, (long long)total_k);
   if (total_q == 0) return M2C_OK;
-  CHECKED(check_rows("q", q, D->q_stride));
-  CHECKED(check_rows("out", out, D->out_stride));
+  CHECKED(check_rows("q", q, D->q_stride, D->head_dim));
+  CHECKED(check_rows("out", out, D->out_stride, D->head_dim));
   if (total_k > 0) {
-    CHECKED(check_rows("k", k, D->k_stride));
-    CHECKED(check_rows("v", v, D->v_stride));
+    CHECKED(check_rows("k", k, D->k_stride, D->head_dim));
+    CHECKED(check_rows("v", v, D->v_stride, D->head_dim));
   }
   CurrentDevice g(D->device);
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", D->device);
@@ -154,8 +161,8 @@ m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
   if (total < 0 || total > kMaxRows || (!cu && total != n))
     return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30], and n without cu", (long long)total);
   if (total == 0) return M2C_OK;
-  CHECKED(check_rows("k", k, k_stride));
-  CHECKED(check_rows("v", v, v_stride));
+  CHECKED(check_rows("k", k, k_stride, C.head_dim));
+  CHECKED(check_rows("v", v, v_stride, C.head_dim));
   CurrentDevice g(cache->device);
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_append(C, seqs, n, cu, total, pos, k, v, k_stride, v_stride,
@@ -172,8 +179,8 @@ m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n
   if (total < 0 || total > kMaxRows)
     return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30]", (long long)total);
   if (total == 0) return M2C_OK;
-  CHECKED(check_rows("k", k, k_stride));
-  CHECKED(check_rows("v", v, v_stride));
+  CHECKED(check_rows("k", k, k_stride, C.head_dim));
+  CHECKED(check_rows("v", v, v_stride, C.head_dim));
   CurrentDevice g(cache->device);
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_read(C, seqs, n, cu, total, k, v, k_stride, v_stride,
@@ -199,8 +206,8 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
   CHECKED(check_heads(cache->dtype, n_heads, C.n_kv_heads, C.head_dim, scale, cache->device));
   if (track != 0 && track != 1) return api_fail(M2C_ERR_INVALID_ARG, "track %d: need 0 or 1", track);
   if (max_len < 0) return api_fail(M2C_ERR_INVALID_ARG, "max_len %d: need >= 0", max_len);
-  CHECKED(check_rows("q", q, q_stride));
-  CHECKED(check_rows("out", out, out_stride));
+  CHECKED(check_rows("q", q, q_stride, C.head_dim));
+  CHECKED(check_rows("out", out, out_stride, C.head_dim));
   const int64_t need = m2c::kv_attend_workspace(C, n, n_heads, track, max_len);
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 255)))
     return api_fail(M2C_ERR_INVALID_ARG, "workspace: need %lld bytes, 256-byte aligned", (long long)need);

@@ -17,12 +17,6 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Weights are taken as 2^(x - m + kLift), l and O alike: rounded to fp16 the
-// largest is 2^14 and those down to 2^-28 of it keep all their bits (2^-14
-// without the lift; a long sequence of small weights beside one large one would
-// lose them). It cancels in O / l and is taken out of the log-sum-exp.
-constexpr float kLift = 14.0f;
-
 // D = A B + C on 16-bit inputs held as raw words. 32x32x16: lane l holds row
 // (column) l % 32 of A (B), elements 8 (l / 32) .. + 7 of the 16 of the sum;
 // D's lane l holds column l % 32, rows 8 (r / 4) + 4 (l / 32) + r % 4.
@@ -103,7 +97,7 @@ __device__ __forceinline__ int64_t item_start(int64_t cu, int b, int per, int mo
   return cu / per + (int64_t)b * more;
 }
 
-// The sequence that owns item x, or -1; every lane of the wave gets it.
+// The sequence that owns item x, or -1 (wave-uniform).
 __device__ __forceinline__ int find_item(const int32_t* cu, int n, int64_t total, int64_t x,
                                          int per, int more) {
   const int lane = threadIdx.x & 63;
@@ -112,9 +106,10 @@ __device__ __forceinline__ int find_item(const int32_t* cu, int n, int64_t total
     const bool at_or_before =
         b < n && item_start(clamp64(cu[b], 0, total), b, per, more) <= x;
     const int cnt = __popcll(__ballot(at_or_before));
-    if (cnt < 64) return base + cnt - 1;  // -1 before the first sequence's items
+    if (cnt < 64)  // -1 before the first sequence's items
+      return __builtin_amdgcn_readfirstlane(base + cnt - 1);
   }
-  return n - 1;
+  return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
 }  // namespace m2c

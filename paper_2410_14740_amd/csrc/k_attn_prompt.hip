@@ -13,6 +13,8 @@
 // operand as they lie: the 8 tokens a lane holds per step of 16 are
 // {4h .. 4h + 3, 8 + 4h .. 8 + 4h + 3} of the 16, h = lane / 32, and V^T's A
 // operand is read in that order (transposing LDS reads, 4 tokens each).
+#include <type_traits>
+
 #include "attn_device.h"
 
 namespace m2c {
@@ -32,22 +34,42 @@ struct PromptArgs {
 namespace {
 
 constexpr int kTileK = 64;  // keys per tile
+// Weights are taken as 2^(x - m + kLift), l and O alike, and m may stay up to
+// kSlack below the largest x. Rounded to fp16 the largest is then 2^14, and
+// weights down to 2^-24 of 2^m keep all their bits (2^-14 without the lift; a
+// long sequence of small weights beside one large one would lose them). It
+// cancels in O / l and is taken out of the log-sum-exp.
+constexpr float kSlack = 4.0f, kLift = 10.0f;
 
-// Zeros for the rows of a tile that are no keys of the sequence (0 * what lies
-// there in memory could be NaN).
-__device__ const u32x4 zero_row[16] = {};
-
-// 16 bytes per lane from global memory straight into LDS (lane i's land at
-// dst + 16 i).
-__device__ __forceinline__ void load_lds16(const uint8_t* src, uint8_t* dst) {
-  __builtin_amdgcn_global_load_lds(
-      (const __attribute__((address_space(1))) void*)(src),
-      (__attribute__((address_space(3))) void*)(dst), 16, 0, 0);
+// A raw buffer over `bytes` bytes at p: loads past its end give zeros.
+__device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
+  const uint64_t a = (uint64_t)(uintptr_t)p;
+  return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, bytes, 0x00020000u};
 }
 
-__device__ __forceinline__ u32x2 read_tr(const uint8_t* lds) {
-  return __builtin_bit_cast(
-      u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(lds)));
+// 16 bytes per lane from buffer offset `off` (per lane) straight into LDS (lane
+// i's land at dst + 16 i, dst the same in every lane). Written out so that the
+// compiler does not wait for it at every LDS read that follows: the loads of
+// one tile run while the tile before it is used, and one explicit wait and a
+// barrier stand between the two.
+__device__ __forceinline__ void load_lds16(u32x4 buf, uint32_t off, uint32_t dst) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %0, 0 offen lds"
+      :
+      : "s"(buf), "v"(off), "s"(dst)
+      : "memory");
+}
+
+// LDS reads by byte address.
+template <typename T>
+__device__ __forceinline__ const __attribute__((address_space(3))) T* lds_at(uint32_t addr) {
+  return (const __attribute__((address_space(3))) T*)(uintptr_t)addr;
+}
+__device__ __forceinline__ u32x2 read_tr(uint32_t addr) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) short4v*)(uintptr_t)addr));
 }
 
 // Tiles lie in LDS as [64][D] 16-bit rows, the 16-byte chunks of a row permuted
@@ -57,7 +79,7 @@ template <int D>
 __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 template <int D>
 __device__ __forceinline__ int swz_v(int row) {
-  return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1;
+  return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
 }
 
 __device__ __forceinline__ float wave_add(float v) {
@@ -70,7 +92,7 @@ __device__ __forceinline__ float wave_add(float v) {
 // taken where a value that some of the rows must not see is an infinity or a
 // NaN, which a product with p = 0 would carry into them.
 template <bool BF, int D>
-__device__ __noinline__ void wave_rows_plain(const PromptArgs& A, const uint8_t* qb, const uint8_t* kb,
+__device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8_t* qb, const uint8_t* kb,
                                              const uint8_t* vb, uint8_t* ob, float* lse, int r0,
                                              int ql, int kl) {
   const int lane = threadIdx.x & 63;
@@ -153,19 +175,22 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
   const int seen = A.causal ? min(kl, max(0, off + row + 1)) : kl;
   const int nt = (wg_seen + kTileK - 1) / kTileK;
 
-  // global -> LDS: load i of a wave takes rows (i NW + wave) kLoadRows .. of a tile
+  // global -> LDS: load i of a wave takes rows (i NW + wave) kLoadRows .. of a
+  // tile; the tile's buffer ends with the sequence, so rows past it are zeros
   const int ld_row = wave * kLoadRows + lane / kChunks;
-  const int ld_ck = ((lane % kChunks) ^ swz_k<D>(ld_row)) * 16;
-  const int ld_cv = ((lane % kChunks) ^ swz_v<D>(ld_row)) * 16;
+  const uint32_t ld_k = (uint32_t)(ld_row * A.k_tok) + ((lane % kChunks) ^ swz_k<D>(ld_row)) * 16;
+  const uint32_t ld_v = (uint32_t)(ld_row * A.v_tok) + ((lane % kChunks) ^ swz_v<D>(ld_row)) * 16;
+  const uint32_t step_k = (uint32_t)(NW * kLoadRows * A.k_tok), step_v = (uint32_t)(NW * kLoadRows * A.v_tok);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0] + wave * 1024;
   auto load_tile = [&](int t, int buf) {
+    const int left = min(kTileK, kl - t * kTileK) - 1;
+    const u32x4 bk = buffer_of(kb + (int64_t)t * kTileK * A.k_tok, (uint32_t)(left * A.k_tok) + kRowBytes);
+    const u32x4 bv = buffer_of(vb + (int64_t)t * kTileK * A.v_tok, (uint32_t)(left * A.v_tok) + kRowBytes);
+    const uint32_t dst = lds0 + buf * (2 * kTileBytes);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int r = t * kTileK + i * NW * kLoadRows + ld_row;
-      const bool in = r < kl;
-      const uint8_t* ks = in ? kb + r * A.k_tok + ld_ck : (const uint8_t*)zero_row;
-      const uint8_t* vs = in ? vb + r * A.v_tok + ld_cv : (const uint8_t*)zero_row;
-      load_lds16(ks, &lds[buf][0][(i * NW + wave) * 1024]);
-      load_lds16(vs, &lds[buf][1][(i * NW + wave) * 1024]);
+      load_lds16(bk, ld_k + i * step_k, dst + i * (NW * 1024));
+      load_lds16(bv, ld_v + i * step_v, dst + kTileBytes + i * (NW * 1024));
     }
   };
 
@@ -174,18 +199,19 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
     const uint8_t* qr = qb + (int64_t)min(row, ql - 1) * A.q_tok + h * 16;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *(const u32x4*)(qr + s * 32);
+    // wait for them here: a wait inside the loop would also wait for its tiles
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
   }
 
-  // LDS read addresses: K row = token col (+ 32), V rows = tokens 4h + i / 4
-  // of a 16-lane group, 16 dimensions from 16 (group & 1)
-  const int k_base = col * kRowBytes, k_x = swz_k<D>(col);
+  // LDS read addresses: K row = token col (+ 32), step ks's chunk 2 ks + h; V
+  // rows = tokens 4h + i / 4 of a 16-lane group, 16 dimensions from 16 (group &
+  // 1) of each 32. The swizzles are xors, so a step is an xor of address bits.
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0];
+  const uint32_t k_lane = lds_base + col * kRowBytes + ((h ^ swz_k<D>(col)) * 16);
   const int vr = 4 * h + ((lane & 15) >> 2);
-  int v_addr[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    const int ch = dt * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-    v_addr[dt] = vr * kRowBytes + (ch ^ swz_v<D>(vr)) * 16 + (lane & 1) * 8;
-  }
+  const uint32_t v_lane = lds_base + kTileBytes + vr * kRowBytes +
+                          (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swz_v<D>(vr)) * 16) + (lane & 1) * 8;
 
   f32x16 o[DT];
 #pragma unroll
@@ -194,90 +220,114 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
   float m = -INFINITY, l = 0.0f;
   uint32_t worst = 0;  // largest |value| bits seen in masked tiles, per half word
-  bool bad = false;
 
-  if (nt > 0) load_tile(0, 0);
-  for (int t = 0; t < nt; ++t) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t + 1 < nt) load_tile(t + 1, (t + 1) & 1);
-    const int k0 = t * kTileK;
-    if (k0 < wv_hi) {
-      const uint8_t* kt = lds[t & 1][0];
-      const uint8_t* vt = lds[t & 1][1];
-      f32x16 s[2];
+  // One tile of keys. MASKED: some row of the wave misses some key of it.
+  auto compute = [&](int t, auto masked_t) {
+    constexpr bool MASKED = decltype(masked_t)::value;
+    const uint32_t buf = (t & 1) * (2 * kTileBytes), ka = k_lane + buf, va = v_lane + buf;
+    f32x16 s[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4 k_0 = *lds_at<u32x4>(ka ^ (ks * 32));
+      const u32x4 k_1 = *lds_at<u32x4>((ka ^ (ks * 32)) + 32 * kRowBytes);
+      s[0] = mfma32<BF>(k_0, qf[ks], s[0]);
+      s[1] = mfma32<BF>(k_1, qf[ks], s[1]);
+    }
+    // four steps' keys ahead of the instructions that take them
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+    for (int ks = 0; ks < KS - 4; ++ks) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+    if constexpr (MASKED) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
+        for (int r = 0; r < 16; ++r)
+          if (t * kTileK + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= seen) s[i][r] = -INFINITY;
+    }
+    float mt = s[0][0];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const int a = k_base + (((ks * 2 + h) ^ k_x) * 16);
-        const u32x4 k_0 = *(const u32x4*)(kt + a);
-        const u32x4 k_1 = *(const u32x4*)(kt + a + 32 * kRowBytes);
-        s[0] = mfma32<BF>(k_0, qf[ks], s[0]);
-        s[1] = mfma32<BF>(k_1, qf[ks], s[1]);
-      }
-      const bool masked = k0 + kTileK > wv_lo;  // some row of the wave misses some key
-      if (masked) {
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (k0 + 32 * i + 8 * (r / 4) + 4 * h + r % 4 >= seen) s[i][r] = -INFINITY;
-      }
-      float mt = s[0][0];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[i][r]);
-      mt = max_xor32(mt) * A.c;  // c > 0
-      const float mn = fmaxf(m, mt), mu = mn == -INFINITY ? 0.0f : mn;
-      const float alpha = exp2_fast(m - mu);
+      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s[i][r]);
+    mt = max_xor32(mt) * A.c;  // c > 0
+    // m follows the largest score only when that is 2^kSlack above it: the
+    // largest weight is then 2^(kLift + kSlack), and most tiles leave l and O as
+    // they are.
+    if (__ballot(mt > m + kSlack)) {
+      const float mn = fmaxf(m, mt);
+      const float alpha = exp2_fast(m - (mn == -INFINITY ? 0.0f : mn));
       m = mn;
-      const float base = mu - kLift;
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[i][r] = exp2_fast(fmaf(s[i][r], A.c, -base));
-          sum += s[i][r];
-        }
-      l = l * alpha + sum;
+      l *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+    }
+    const float base = (m == -INFINITY ? 0.0f : m) - kLift;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        u32x4 p;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          p[w] = pack16<BF>(s[u / 2][(u & 1) * 8 + 2 * w], s[u / 2][(u & 1) * 8 + 2 * w + 1]);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const u32x2 lo = read_tr(vt + v_addr[dt] + (16 * u) * kRowBytes);
-          const u32x2 hi = read_tr(vt + v_addr[dt] + (16 * u + 8) * kRowBytes);
-          const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
-          if (masked) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-              worst = __builtin_bit_cast(
-                  uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, worst),
-                                                      __builtin_bit_cast(us2, vf[w] & 0x7fff7fffu)));
-            }
-          }
-          o[dt] = mfma32<BF>(vf, p, o[dt]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        s[i][r] = exp2_fast(fmaf(s[i][r], A.c, -base));
+        sum[r & 3] += s[i][r];
       }
-      if (masked) {
-        constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
-        bad = bad || __ballot((worst & 0xffffu) >= kInf || (worst >> 16) >= kInf) != 0;
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      u32x4 p;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        p[w] = pack16<BF>(s[u / 2][(u & 1) * 8 + 2 * w], s[u / 2][(u & 1) * 8 + 2 * w + 1]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x2 lo = read_tr((va ^ (dt * 64)) + (16 * u) * kRowBytes);
+        const u32x2 hi = read_tr((va ^ (dt * 64)) + (16 * u + 8) * kRowBytes);
+        const u32x4 vf = {lo[0], lo[1], hi[0], hi[1]};
+        if constexpr (MASKED) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+            worst = __builtin_bit_cast(
+                uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, worst),
+                                                    __builtin_bit_cast(us2, vf[w] & 0x7fff7fffu)));
+          }
+        }
+        o[dt] = mfma32<BF>(vf, p, o[dt]);
       }
     }
+  };
+
+  // Waves pass the barriers of the two loops together, each with its own number
+  // of tiles in the first.
+  if (nt > 0) load_tile(0, 0);
+  const int plain = r0 >= ql ? 0 : wv_lo / kTileK;  // tiles that every row of the wave sees whole
+  auto arrive = [&](int t) {
+    // this wave's part of tile t has landed and its reads of tile t - 1 are done
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (t + 1 < nt) load_tile(t + 1, (t + 1) & 1);
+  };
+  int t = 0;
+  for (; t < plain; ++t) {
+    arrive(t);
+    compute(t, std::false_type());
   }
+  for (; t < nt; ++t) {
+    arrive(t);
+    if (t * kTileK < wv_hi) compute(t, std::true_type());
+  }
+  constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
+  const bool bad = __ballot((worst & 0xffffu) >= kInf || (worst >> 16) >= kInf) != 0;
   if (r0 >= ql) return;
   if (bad && A.causal) {
     wave_rows_plain<BF, D>(A, qb, kb, vb, ob, lse, r0, ql, kl);

@@ -45,6 +45,12 @@ namespace {
 
 constexpr int kWaves = 4;
 
+// Weights are taken as 2^(x - m + kLift), l and O alike: rounded to fp16 the
+// largest is 2^14 and those down to 2^-28 of it keep all their bits (2^-14
+// without the lift; a long sequence of small weights beside one large one would
+// lose them). It cancels in O / l and is taken out of the log-sum-exp.
+constexpr float kLift = 14.0f;
+
 // p of a unit's tokens from its scores, and the running statistics. s: scores
 // in units of 2^ (masked ones -infinity). Returns the factor for what was
 // summed before; *unit_sum the lane's sum of p.
