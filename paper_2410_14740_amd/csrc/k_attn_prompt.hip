@@ -28,7 +28,6 @@ struct PromptArgs {
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // bytes
   float c;     // scale * log2 e
   int n_seqs, n_heads, group, causal;
-  int items;   // tiles of query rows over all sequences (find_item)
 };
 
 namespace {
@@ -128,6 +127,45 @@ __device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8
   }
 }
 
+// The sequence and tile of query rows of tile index x, or -1. Workgroups start
+// in index order, and a tile costs what its rows see: sequences go by their
+// keys, longest first, and in each a causal mask's longest rows first, so that
+// the last workgroups to start are short ones. More than 64 sequences (a lane
+// each) are taken as they come.
+template <int ROWS>
+__device__ __forceinline__ int find_tile(const PromptArgs& A, int x, int* qt) {
+  const int lane = threadIdx.x & 63, n = A.n_seqs;
+  int b, j, tiles;
+  if (n <= 64) {
+    int kl = -1, nt = 0;
+    if (lane < n) {
+      const int64_t lo = clamp64(A.cu_q[lane], 0, A.total_q), hi = clamp64(A.cu_q[lane + 1], lo, A.total_q);
+      const int64_t k0 = clamp64(A.cu_k[lane], 0, A.total_k), k1 = clamp64(A.cu_k[lane + 1], k0, A.total_k);
+      nt = (int)((hi - lo + ROWS - 1) / ROWS);
+      kl = (int)(k1 - k0);
+    }
+    int start = 0;  // tiles of the sequences before the lane's
+    for (int i = 0; i < n; ++i) {
+      const int k2 = __builtin_amdgcn_readlane(kl, i), n2 = __builtin_amdgcn_readlane(nt, i);
+      if (k2 > kl || (k2 == kl && i < lane)) start += n2;
+    }
+    const unsigned long long own = __ballot(x >= start && x < start + nt);
+    if (!own) return -1;
+    b = __builtin_amdgcn_readfirstlane(__ffsll(own) - 1);
+    j = x - __builtin_amdgcn_readlane(start, b);
+    tiles = __builtin_amdgcn_readlane(nt, b);
+  } else {
+    b = find_item(A.cu_q, n, A.total_q, x, ROWS, 1);
+    if (b < 0) return -1;
+    const int64_t lo = clamp64(A.cu_q[b], 0, A.total_q), hi = clamp64(A.cu_q[b + 1], lo, A.total_q);
+    tiles = (int)((hi - lo + ROWS - 1) / ROWS);
+    j = x - (int)item_start(lo, b, ROWS, 1);
+    if (j >= tiles) return -1;
+  }
+  *qt = A.causal ? tiles - 1 - j : j;
+  return b;
+}
+
 template <bool BF, int D, int NW>
 __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const PromptArgs A) {
   constexpr int kRows = NW * 32;           // query rows per workgroup
@@ -138,24 +176,20 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
   constexpr int KS = D / 16, DT = D / 32;
   __shared__ __align__(1024) uint8_t lds[2][2][kTileBytes];
 
-  // The items of one key/value head follow each other and go to one XCD
-  // (consecutive workgroups go round the eight), so that its L2 serves the
-  // head's keys and values to all of them.
-  const int G = A.group, per_kv = A.items * G, total = per_kv * (A.n_heads / G);
-  const int per_xcd = (total + 7) / 8;
-  const int item = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if (item >= total) return;
-  const int kvh = item / per_kv, in_kv = item - kvh * per_kv;
-  const int x = in_kv / G, head = kvh * G + (in_kv - x * G);
-  const int b = find_item(A.cu_q, A.n_seqs, A.total_q, x, kRows, 1);
+  // Consecutive workgroups go round the eight XCDs: they take the heads of one
+  // query tile, and where the key/value heads divide by eight, each XCD keeps
+  // the same ones, so that its L2 holds their keys and values for all tiles.
+  const int G = A.group, n_kv = A.n_heads / G;
+  const int x = blockIdx.x / A.n_heads, r = blockIdx.x - x * A.n_heads;
+  const int per_xcd = n_kv / 8;
+  const int hr = n_kv % 8 == 0 ? (r & 7) * per_xcd * G + (r >> 3) : r;
+  const int kvh = hr / G, head = hr;
+  int qt;
+  const int b = find_tile<kRows>(A, x, &qt);
   if (b < 0) return;
   const int64_t q_lo = clamp64(A.cu_q[b], 0, A.total_q), q_hi = clamp64(A.cu_q[b + 1], q_lo, A.total_q);
   const int64_t k_lo = clamp64(A.cu_k[b], 0, A.total_k), k_hi = clamp64(A.cu_k[b + 1], k_lo, A.total_k);
   const int ql = (int)(q_hi - q_lo), kl = (int)(k_hi - k_lo);
-  const int n_tiles = (ql + kRows - 1) / kRows;
-  const int j = x - (int)item_start(q_lo, b, kRows, 1);
-  if (j >= n_tiles) return;
-  const int qt = A.causal ? n_tiles - 1 - j : j;  // longest rows first
 
   const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -352,9 +386,8 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
 template <bool BF, int D, int NW>
 hipError_t launch_tile(PromptArgs& A, hipStream_t stream) {
   const int64_t items = A.total_q / (NW * 32) + A.n_seqs;
-  const int64_t grid = (items * A.n_heads + 7) / 8 * 8;
+  const int64_t grid = items * A.n_heads;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  A.items = (int)items;
   hipLaunchKernelGGL((prompt_attention_kernel<BF, D, NW>), dim3((uint32_t)grid), dim3(NW * 64), 0,
                      stream, A);
   return hipGetLastError();

@@ -115,17 +115,18 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   const int b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
   const int heads = min(16, A.group - ht * 16);           // query heads of this tile
   const int h0 = kvh * A.group + ht * 16;                 // the first
-  const int BT = C.block_tokens, per_block = BT / UNIT;
+  const int BT = C.block_tokens;
+  const int halves = BT / UNIT - 1;  // a block is one unit, or two: 0 or 1
   const int s_id = A.seqs ? A.seqs[b] : b;
   const bool known = s_id >= 0 && s_id < C.n_seqs;
   const int s = known ? s_id : 0;
   if (!known && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
   const int len = known ? (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * BT) : 0;
-  const int full = len / BT * per_block;                  // units that lie in pages
+  const int full = (len / BT) << halves;                  // units that lie in pages
   const int units = full + (len - len / BT * BT + UNIT - 1) / UNIT;
   const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
   const int32_t* table = C.table + sh * C.max_blocks;
-  float2* wsum = A.wsum ? A.wsum + ((int64_t)rk * C.max_blocks * per_block) * A.group + ht * 16 + col
+  float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
                         : nullptr;
 
   // queries: column = head, a step's elements where the key loads have them
@@ -166,33 +167,33 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   for (int u0 = split * A.chunk; u0 < units; u0 += A.splits * A.chunk) {
     const int u1 = min(units, u0 + A.chunk);
     // A wave's units of the chunk are u0 + wave, + kWaves, .. (at most 64);
-    // lane i holds the page and scales of its i-th.
+    // lane i holds the page of its i-th, -1 for one that does not exist: page 0
+    // stands in with scales of 0, a block of zeros.
     const int mine = u0 + wave + kWaves * lane;
     int page = 0;
-    float sk = 0.0f, sv = 0.0f;
     if (mine < min(u1, full)) {
-      page = table[mine / per_block];
+      page = table[mine >> halves];
       if (page < 0 || page >= C.n_pages) {
         atomicOr(C.status, kKvBadIndex);
-        page = 0;  // in bounds; a scale of 0 makes a block of zeros of it
-      } else {
-        sk = C.k_scale[page];
-        sv = C.v_scale[page];
+        page = -1;
       }
     }
-    for (int u = u0 + wave, i = 0; u < min(u1, full); u += kWaves, ++i) {
-      const int pg = __builtin_amdgcn_readlane(page, i);
-      const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sk), i));
-      const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sv), i));
-      const int64_t at = ((int64_t)pg * BT + (u % per_block) * UNIT) * D;
+    // Each register set is loaded for the next unit as soon as the products have
+    // taken it, so a wave keeps up to a unit's bytes in flight while it computes.
+    u32x4 kw[T][KL];
+    uint32_t vw[V2][8][VW];
+    auto unit_at = [&](int u, int pg) {
+      return ((int64_t)max(pg, 0) * BT + (u & halves) * UNIT) * D;
+    };
+    auto load_k = [&](int64_t at) {
       const int8_t* kp = C.k_codes + at + col * D + qr * 16;
-      const int8_t* vp = C.v_codes + at + qr * 4 * D + col * E;
-      u32x4 kw[T][KL];
-      uint32_t vw[V2][8][VW];
 #pragma unroll
       for (int t = 0; t < T; ++t)
 #pragma unroll
         for (int k = 0; k < KL; ++k) kw[t][k] = *(const u32x4*)(kp + t * 16 * D + k * 64);
+    };
+    auto load_v = [&](int64_t at) {
+      const int8_t* vp = C.v_codes + at + qr * 4 * D + col * E;
 #pragma unroll
       for (int v = 0; v < V2; ++v)
 #pragma unroll
@@ -205,6 +206,16 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
             vw[v][j][0] = *(const uint32_t*)p;
           }
         }
+    };
+    // Scales come by scalar loads: a wait for them does not wait for the pages.
+    typedef const __attribute__((address_space(4))) float* Scales;
+    const Scales k_scale = (Scales)(uintptr_t)C.k_scale, v_scale = (Scales)(uintptr_t)C.v_scale;
+    // One unit, page pg; MORE: then loads the one at `next`. (The last unit is a
+    // copy of the code, not a condition in it: where a load may be left out the
+    // compiler has to wait for all that may be in flight.)
+    auto process = [&](int u, int pg, int64_t next, auto more_t) {
+      constexpr bool MORE = decltype(more_t)::value;
+      const float ks = pg < 0 ? 0.0f : k_scale[pg], vs = pg < 0 ? 0.0f : v_scale[pg];
       f32x4 x[T];
       const float f = ks * qc;
 #pragma unroll
@@ -222,98 +233,122 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[t][r] *= f;
       }
+      if constexpr (MORE) load_k(next);
+      asm volatile("" ::: "memory");
       float sum;
       const float alpha = softmax_step<T>(x, m, l, &sum);
       if (wsum) {
         sum = add_xor16(add_xor32(sum));
         if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
       }
-      f32x4 acc[E];
+      u32x4 pf[V2];
 #pragma unroll
-      for (int i2 = 0; i2 < E; ++i2) acc[i2] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int v = 0; v < V2; ++v) pf[v] = pack_p<false>(x[2 * v], x[2 * v + 1]);
 #pragma unroll
-      for (int v = 0; v < V2; ++v) {
-        const u32x4 pf = pack_p<false>(x[2 * v], x[2 * v + 1]);
+      for (int w = 0; w < VW; ++w) {
+        f32x4 acc[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int v = 0; v < V2; ++v) {
+          uint32_t c[8];
 #pragma unroll
-          for (int w = 0; w < VW; ++w) vw[v][j][w] ^= 0x80808080u;
-#pragma unroll
-        for (int w = 0; w < VW; ++w) {
+          for (int j = 0; j < 8; ++j) c[j] = vw[v][j][w] ^ 0x80808080u;
           auto frag = [&](auto idx) {
             constexpr int I = decltype(idx)::value;
-            const u32x4 vf = {pair_of<I>(vw[v][0][w], vw[v][1][w]), pair_of<I>(vw[v][2][w], vw[v][3][w]),
-                              pair_of<I>(vw[v][4][w], vw[v][5][w]), pair_of<I>(vw[v][6][w], vw[v][7][w])};
-            acc[w * 4 + I] = mfma16<false>(vf, pf, acc[w * 4 + I]);
+            const u32x4 vf = {pair_of<I>(c[0], c[1]), pair_of<I>(c[2], c[3]), pair_of<I>(c[4], c[5]),
+                              pair_of<I>(c[6], c[7])};
+            acc[I] = mfma16<false>(vf, pf[v], v == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[I]);
           };
           frag(std::integral_constant<int, 0>());
           frag(std::integral_constant<int, 1>());
           frag(std::integral_constant<int, 2>());
           frag(std::integral_constant<int, 3>());
         }
+#pragma unroll
+        for (int i2 = 0; i2 < 4; ++i2)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            o[w * 4 + i2][r] = fmaf(acc[i2][r], vs, o[w * 4 + i2][r] * alpha);
       }
-#pragma unroll
-      for (int i2 = 0; i2 < E; ++i2)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[i2][r] = fmaf(acc[i2][r], vs, o[i2][r] * alpha);
+      if constexpr (MORE) load_v(next);
+    };
+    const int end = min(u1, full);
+    if (u0 + wave < end) {
+      int pg = __builtin_amdgcn_readlane(page, 0);
+      const int64_t at = unit_at(u0 + wave, pg);
+      load_k(at);
+      asm volatile("" ::: "memory");  // in this order, so that a wait for the keys is for them alone
+      load_v(at);
+      int u = u0 + wave;
+      for (int i = 1; u + kWaves < end; u += kWaves, ++i) {
+        const int next = __builtin_amdgcn_readlane(page, i);
+        process(u, pg, unit_at(u + kWaves, next), std::true_type());
+        pg = next;
+      }
+      process(u, pg, 0, std::false_type());
     }
-    // units of the open block, from the 16-bit tail; rows past the length are
-    // zeros, whatever the tail holds there
-    for (int u = u0 + wave; u < u1; u += kWaves) {
-      if (u < full) continue;
-      const int t_first = u * UNIT - len / BT * BT, left = len % BT - t_first;
-      const uint8_t* kt = C.tail_k + (sh * BT + t_first) * (D * 2);
-      const uint8_t* vt = C.tail_v + (sh * BT + t_first) * (D * 2);
-      f32x4 x[T];
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const bool in = t * 16 + col < left;
+    // Units of the open block, from the 16-bit tail, 32 tokens at a time; rows
+    // past the length are zeros, whatever the tail holds there.
+    for (int u = max(u0 + wave, full + ((u0 + wave - full) & (kWaves - 1))); u < u1; u += kWaves) {
+      const int t_first = (u - full) * UNIT, rest = min(UNIT, len % BT - t_first);
+      float sum = 0.0f;
+#pragma unroll 1
+      for (int part = 0; part < rest; part += 32) {
+        const int left = rest - part;
+        const uint8_t* kt = C.tail_k + (sh * BT + t_first + part) * (D * 2);
+        const uint8_t* vt = C.tail_v + (sh * BT + t_first + part) * (D * 2);
+        // every load is issued before the first is used, from the last token
+        // where there is none
+        typedef uint32_t Row __attribute__((ext_vector_type(E / 2)));
+        u32x4 qw[KS], kl[2][KS];
+        Row vl[8];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           const int el = (k / 2) * 64 + qr * 16 + (k & 1) * 8;
-          const u32x4 qw = *(const u32x4*)(qrow + el * 2);
-          const u32x4 kf = in ? *(const u32x4*)(kt + ((t * 16 + col) * D + el) * 2) : u32x4{0, 0, 0, 0};
-          x[t] = mfma16<BF>(kf, qw, x[t]);
+          qw[k] = *(const u32x4*)(qrow + el * 2);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            kl[t][k] = *(const u32x4*)(kt + (min(t * 16 + col, left - 1) * D + el) * 2);
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          x[t][r] = t * 16 + qr * 4 + r < left ? x[t][r] * A.c : -INFINITY;
-      }
-      float sum;
-      const float alpha = softmax_step<T>(x, m, l, &sum);
-      if (wsum) {
-        sum = add_xor16(add_xor32(sum));
-        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
-      }
+        for (int j = 0; j < 8; ++j)
+          vl[j] = *(const Row*)(vt + (min((j / 4) * 16 + qr * 4 + j % 4, left - 1) * D + col * E) * 2);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 x[2];
 #pragma unroll
-      for (int i = 0; i < E; ++i)
+        for (int t = 0; t < 2; ++t) {
+          x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          const bool in = t * 16 + col < left;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
+          for (int k = 0; k < KS; ++k)
+            x[t] = mfma16<BF>(in ? kl[t][k] : u32x4{0, 0, 0, 0}, qw[k], x[t]);
 #pragma unroll
-      for (int v = 0; v < V2; ++v) {
-        const u32x4 pf = pack_p<BF>(x[2 * v], x[2 * v + 1]);
-        uint32_t w[8][E / 2];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tok = v * 32 + (j / 4) * 16 + qr * 4 + j % 4;
-#pragma unroll
-          for (int e = 0; e < E / 2; ++e) w[j][e] = 0;
-          if (tok < left) {
-            const uint32_t* p = (const uint32_t*)(vt + (tok * D + col * E) * 2);
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) w[j][e] = p[e];
-          }
+          for (int r = 0; r < 4; ++r)
+            x[t][r] = t * 16 + qr * 4 + r < left ? x[t][r] * A.c : -INFINITY;
         }
+        float part_sum;
+        const float alpha = softmax_step<2>(x, m, l, &part_sum);
+        sum = sum * alpha + part_sum;
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
+        const u32x4 pf = pack_p<BF>(x[0], x[1]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if ((j / 4) * 16 + qr * 4 + j % 4 >= left) vl[j] = Row{};
 #pragma unroll
         for (int i = 0; i < E; ++i) {
           const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-          const u32x4 vf = {__builtin_amdgcn_perm(w[1][i / 2], w[0][i / 2], sel),
-                            __builtin_amdgcn_perm(w[3][i / 2], w[2][i / 2], sel),
-                            __builtin_amdgcn_perm(w[5][i / 2], w[4][i / 2], sel),
-                            __builtin_amdgcn_perm(w[7][i / 2], w[6][i / 2], sel)};
+          const u32x4 vf = {__builtin_amdgcn_perm(vl[1][i / 2], vl[0][i / 2], sel),
+                            __builtin_amdgcn_perm(vl[3][i / 2], vl[2][i / 2], sel),
+                            __builtin_amdgcn_perm(vl[5][i / 2], vl[4][i / 2], sel),
+                            __builtin_amdgcn_perm(vl[7][i / 2], vl[6][i / 2], sel)};
           o[i] = mfma16<BF>(vf, pf, o[i]);
         }
+      }
+      if (wsum) {
+        sum = add_xor16(add_xor32(sum));
+        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
       }
     }
   }

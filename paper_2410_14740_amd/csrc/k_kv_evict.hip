@@ -129,7 +129,6 @@ __global__ void __launch_bounds__(NT) evict_kernel(const KvView C, const int32_t
     if (head == 0 && tid == 0) len_out[s] = len - gone * BT;
   } else if (tid == 0) {
     // the last head's workgroup to get here writes the length that all have read
-    __threadfence();
     if (atomicAdd(&C.arrive[s], 1) == C.n_kv_heads - 1) {
       C.arrive[s] = 0;
       C.len[s] = len - gone * BT;

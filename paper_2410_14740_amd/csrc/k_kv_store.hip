@@ -15,24 +15,81 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t a, uint32_t b) {
                                                                 __builtin_bit_cast(us2, b)));
 }
 
-// code = clamp(rne(x / s), -127, 127) with the fp32 quotient; 0 where the scale
-// is 0 or not finite.
-__device__ __forceinline__ uint32_t code8(float x, float s) {
-  const float r = fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.0f), 127.0f);
-  return (uint32_t)(int)r & 0xffu;
+// Codes of a chunk of 8 elements: rne of the correctly rounded fp32 quotient x /
+// s, as two words. With r the rounded 1 / s, q = x r and one correction by the
+// exact remainder give that quotient (three operations instead of a division's
+// dozen, which would take longer than the memory); the tests compare every pair
+// of fp16 and of bf16 significands. Adding 1.5 2^23 rounds it to an integer, ties
+// to even, in the low byte. |x| <= 127 s (1 + 2^-23), so nothing has to be
+// clamped.
+template <bool BF>
+__device__ __forceinline__ u32x2 codes_of(u32x4 x, float s, float r) {
+  uint32_t t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = unpack16<BF>(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xffffu);
+    const float q = v * r;
+    t[i] = __float_as_uint(fmaf(fmaf(-q, s, v), r, q) + 12582912.0f);
+  }
+  u32x2 c;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    c[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[4 * i + 3], t[4 * i + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(t[4 * i + 1], t[4 * i], 0x0c0c0400u), 0x05040100u);
+  return c;
 }
 
+// The same by a division, for scales whose reciprocal is not a normal number
+// (bf16 blocks below 2^-93 or above 2^107).
 template <bool BF>
-__device__ __forceinline__ u32x2 codes_of(u32x4 x, float s, bool any) {
+__device__ __forceinline__ u32x2 codes_divided(u32x4 x, float s) {
   u32x2 c = {0, 0};
-  if (any) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t a = code8(unpack16<BF>(x[w] & 0xffffu), s), b = code8(unpack16<BF>(x[w] >> 16), s);
-      c[w / 2] |= (a | b << 8) << (16 * (w & 1));
-    }
+  for (int i = 0; i < 8; ++i) {
+    const float v = unpack16<BF>(i & 1 ? x[i / 2] >> 16 : x[i / 2] & 0xffffu);
+    const uint32_t t = __float_as_uint(__fdiv_rn(v, s) + 12582912.0f) & 0xffu;
+    c[i / 4] |= t << (8 * (i & 3));
   }
   return c;
+}
+
+// A thread's chunks of a block (see append_kernel) as codes. A block without a
+// magnitude, or with one that is not finite, has codes 0.
+template <bool BF, int D, int BT>
+__device__ __forceinline__ void store_codes(int8_t* page, const u32x4 (&x)[BT * D / 2048], float s) {
+  u32x2* to = (u32x2*)page + threadIdx.x;
+  const bool normal = s >= 0x1p-100f && s <= 0x1p100f;
+  const float r = __fdiv_rn(1.0f, s);
+  if (normal) {
+#pragma unroll
+    for (int i = 0; i < BT * D / 2048; ++i) to[i * 256] = codes_of<BF>(x[i], s, r);
+  } else {
+    const bool any = s > 0.0f && s < INFINITY;
+#pragma unroll
+    for (int i = 0; i < BT * D / 2048; ++i) to[i * 256] = any ? codes_divided<BF>(x[i], s) : u32x2{0, 0};
+  }
+}
+
+// Where an append of nb tokens goes: from p0 to end, if that is a place of the
+// sequence (the start of a block, or in the last block) and it fits.
+struct Place {
+  int p0, end;
+  bool placed, fits;
+};
+
+__device__ __forceinline__ Place place_of(const KvView& C, int s, const int32_t* pos, int nb) {
+  const int BT = C.block_tokens, len = C.len[s];
+  Place p;
+  p.p0 = pos ? *pos : len;
+  p.placed = p.p0 >= 0 && p.p0 <= len && (p.p0 % BT == 0 || p.p0 / BT == (len - 1) / BT);
+  p.fits = (int64_t)p.p0 + nb <= (int64_t)C.max_blocks * BT;
+  p.end = p.fits ? p.p0 + nb : 0;
+  return p;
+}
+
+__device__ __forceinline__ void set_length(const KvView& C, int s, bool placed, bool fits, int end) {
+  if (placed && fits) C.len[s] = end;
+  else atomicOr(C.status, placed ? kKvCapacity : kKvState);
 }
 
 // One block of one sequence and key/value head. Thread t holds chunk t % (D/8)
@@ -67,12 +124,9 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
     if (tid == 0) atomicOr(C.status, kKvBadIndex);
     return;
   }
-  const int len = C.len[s];
-  const int p0 = pos ? pos[b] : len;
-  const bool placed = p0 >= 0 && p0 <= len && (p0 % BT == 0 || p0 / BT == (len - 1) / BT);
-  const bool fits = (int64_t)p0 + nb <= (int64_t)C.max_blocks * BT;
-  const int end = p0 + nb;
-  if (placed && fits) {
+  const Place p = place_of(C, s, pos ? &pos[b] : nullptr, nb);
+  const int p0 = p.p0, end = p.end;
+  if (p.placed && p.fits) {
     const int first = p0 / BT, last = (end - 1) / BT;
     const int64_t sh = (int64_t)s * C.n_kv_heads + head;
     uint8_t* tk = C.tail_k + sh * BT * (D * 2);
@@ -86,6 +140,7 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
       const int at = blk * BT;  // first token of the block
       if (tid == 0 && at >= p0) C.weight[sh * C.max_blocks + blk] = 0.0f;
       if (at + BT > end) continue;  // stays open
+      const int page = C.table[sh * C.max_blocks + blk];
       u32x4 xk[NP], xv[NP];
       uint32_t mk = 0, mv = 0;
 #pragma unroll
@@ -118,20 +173,12 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
       mv = max_mag(max_mag(mags[1][0], mags[1][1]), max_mag(mags[1][2], mags[1][3]));
       const float sk = __fdiv_rn(unpack16<BF>(max(mk & 0xffffu, mk >> 16)), 127.0f);
       const float sv = __fdiv_rn(unpack16<BF>(max(mv & 0xffffu, mv >> 16)), 127.0f);
-      const int page = C.table[sh * C.max_blocks + blk];
       if (page < 0 || page >= C.n_pages) {
         if (tid == 0) atomicOr(C.status, kKvBadIndex);
         continue;
       }
-      const bool ak = sk > 0.0f && sk < INFINITY, av = sv > 0.0f && sv < INFINITY;
-      int8_t* ck = C.k_codes + (int64_t)page * (BT * D);
-      int8_t* cv = C.v_codes + (int64_t)page * (BT * D);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int t = t0 + i * TP;
-        *(u32x2*)(ck + t * D + ch * 8) = codes_of<BF>(xk[i], sk, ak);
-        *(u32x2*)(cv + t * D + ch * 8) = codes_of<BF>(xv[i], sv, av);
-      }
+      store_codes<BF, D, BT>(C.k_codes + (int64_t)page * (BT * D), xk, sk);
+      store_codes<BF, D, BT>(C.v_codes + (int64_t)page * (BT * D), xv, sv);
       if (tid == 0) {
         C.k_scale[page] = sk;
         C.v_scale[page] = sv;
@@ -148,17 +195,29 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
       }
     }
   }
-  // Every thread of every workgroup of the sequence has read the length before
-  // the workgroup arrives; the last one to arrive writes the new one.
+  // The new length is written when every workgroup of the sequence has read the
+  // old one: with one token each, by the last of the heads' workgroups to
+  // arrive; with many workgroups, whose arrivals at one counter would take
+  // longer (25 ns each) than the memory, by a second launch.
+  if (cu) return;
   __syncthreads();
-  if (tid == 0) {
-    __threadfence();
-    if (atomicAdd(&C.arrive[s], 1) == items * C.n_kv_heads - 1) {
-      C.arrive[s] = 0;
-      if (placed && fits) C.len[s] = end;
-      else atomicOr(C.status, placed ? kKvCapacity : kKvState);
-    }
+  if (tid == 0 && atomicAdd(&C.arrive[s], 1) == C.n_kv_heads - 1) {
+    C.arrive[s] = 0;
+    set_length(C, s, p.placed, p.fits, p.end);
   }
+}
+
+__global__ void __launch_bounds__(256) length_kernel(const KvView C, const int32_t* seqs, int n,
+                                                     const int32_t* cu, int64_t total,
+                                                     const int32_t* pos) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= n) return;
+  const int64_t row0 = clamp64(cu[b], 0, total);
+  const int nb = (int)(clamp64(cu[b + 1], row0, total) - row0);
+  const int s = seqs ? seqs[b] : b;
+  if (nb == 0 || s < 0 || s >= C.n_seqs) return;
+  const Place p = place_of(C, s, pos ? &pos[b] : nullptr, nb);
+  set_length(C, s, p.placed, p.fits, p.end);
 }
 
 template <bool BF, int D, int BT>
@@ -261,13 +320,16 @@ hipError_t launch_kv_append(const KvView& C, const int32_t* seqs, int n, const i
                             const int64_t* ks, const int64_t* vs, hipStream_t stream) {
   const int64_t items = cu ? total / C.block_tokens + 2 * (int64_t)n : n;
   if (items * C.n_kv_heads > INT32_MAX) return hipErrorInvalidValue;
-  return by_shape(C, [&](auto bf, auto d, auto bt) {
+  const hipError_t e = by_shape(C, [&](auto bf, auto d, auto bt) {
     hipLaunchKernelGGL((append_kernel<decltype(bf)::value, decltype(d)::value, decltype(bt)::value>),
                        dim3((uint32_t)(items * C.n_kv_heads)), dim3(256), 0, stream, C, seqs, n, cu,
                        total, pos, (const uint8_t*)k, (const uint8_t*)v, ks[0] * 2, ks[1] * 2,
                        vs[0] * 2, vs[1] * 2);
     return hipGetLastError();
   });
+  if (e != hipSuccess || !cu) return e;
+  hipLaunchKernelGGL(length_kernel, dim3((n + 255) / 256), dim3(256), 0, stream, C, seqs, n, cu, total, pos);
+  return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,
