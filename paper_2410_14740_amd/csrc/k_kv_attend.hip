@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
                         : nullptr;
 
+  if (A.splits > 1 && split * A.chunk >= units) return;  // a split without tokens; the join knows
   // queries: column = head, a step's elements where the key loads have them
   u32x4 qf[KS];
   const uint8_t* qrow = A.q + b * A.q_row + (h0 + min(col, heads - 1)) * A.q_head;
@@ -400,22 +401,29 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
 
 // Joins the splits of one query head: 256 threads, D / 4 of them per split.
 template <bool BF, int D>
-__global__ void __launch_bounds__(256) join_kernel(const AttendArgs A) {
+__global__ void __launch_bounds__(256) join_kernel(const AttendArgs A, int unit) {
   constexpr int TS = D / 4, GR = 256 / TS;
   __shared__ __align__(16) f32x4 acc[GR][TS];
   const int tid = threadIdx.x;
   const int64_t at = blockIdx.x;
+  const int b = (int)(at / A.n_heads), h = (int)(at - (int64_t)b * A.n_heads);
+  const int s_id = A.seqs ? A.seqs[b] : b;
+  const KvView& C = A.C;
+  const int len = s_id >= 0 && s_id < C.n_seqs
+                      ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * C.block_tokens) : 0;
+  const int used = min(A.splits, (len + A.chunk * unit - 1) / (A.chunk * unit));  // splits with tokens
   const float2* ml = A.part_ml + at * A.splits;
   float M = -INFINITY, L = 0.0f;
-  for (int s = tid & 63; s < A.splits; s += 64) M = fmaxf(M, ml[s].x);
+  for (int s = tid & 63; s < used; s += 64) M = fmaxf(M, ml[s].x);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
   const float mu = M == -INFINITY ? 0.0f : M;
-  for (int s = tid & 63; s < A.splits; s += 64) L += ml[s].y * exp2_fast(ml[s].x - mu);
+  for (int s = tid & 63; s < used; s += 64) L += ml[s].y * exp2_fast(ml[s].x - mu);
   L = wave_sum(L);
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
   const float* po = A.part_o + at * A.splits * D + (tid % TS) * 4;
-  for (int s = tid / TS; s < A.splits; s += GR) {
+#pragma unroll 4
+  for (int s = tid / TS; s < used; s += GR) {
     const float f = exp2_fast(ml[s].x - mu);
     const f32x4 v = *(const f32x4*)(po + (int64_t)s * D);
 #pragma unroll
@@ -429,7 +437,6 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs A) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] += acc[g][tid][i];
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  const int64_t b = at / A.n_heads, h = at - b * A.n_heads;
   uint32_t* out = (uint32_t*)(A.out + b * A.o_row + h * A.o_head + tid * 8);
   out[0] = pack16<BF>(y[0] * inv, y[1] * inv);
   out[1] = pack16<BF>(y[2] * inv, y[3] * inv);
@@ -465,6 +472,8 @@ __global__ void __launch_bounds__(256) weigh_kernel(const AttendArgs A, int unit
 
 int unit_of(const KvView& C) { return C.block_tokens < 64 ? 32 : 64; }
 
+constexpr int kMaxSplits = 1024;
+
 struct Split {
   int tiles, splits, chunk;
 };
@@ -477,10 +486,15 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   Split S;
   S.tiles = (group + 15) / 16;
   const int64_t rows = (int64_t)n * C.n_kv_heads * S.tiles;
-  int64_t chunk = (rows * units + 2047) / 2048;
+  // 512 workgroups run at once (two per CU). Up to 32 units each, one round of
+  // them covers the call; more come in rounds of 16 units, shorter ones, so that
+  // the last round's end is ragged by less. (131071 tokens x 8 heads, 8 / 16 /
+  // 32 / 48 units: 48, 45, 44, 53 us and a join of 20, 11, 6, 6; 32 sequences of
+  // 500 .. 23254 tokens x 8 heads: 167, 150, 160, 200 us.)
+  int64_t chunk = (rows * units + 511) / 512;
+  if (chunk > 32) chunk = 16;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
-  chunk = chunk < 8 ? 8 : chunk > 64 ? 64 : chunk;
-  while ((units + chunk - 1) / chunk > 1024) chunk += kWaves;
+  while ((units + chunk - 1) / chunk > kMaxSplits) chunk += kWaves;
   S.chunk = (int)chunk;
   S.splits = (int)((units + chunk - 1) / chunk);
   if (S.splits < 1) S.splits = 1;
@@ -540,7 +554,7 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
 #define M2C_ATTEND(BF, D, U) \
   hipLaunchKernelGGL((attend_kernel<BF, D, U>), dim3((uint32_t)grid), dim3(kWaves * 64), 0, stream, A)
 #define M2C_JOIN(BF, D) \
-  hipLaunchKernelGGL((join_kernel<BF, D>), dim3((uint32_t)((int64_t)n * n_heads)), dim3(256), 0, stream, A)
+  hipLaunchKernelGGL((join_kernel<BF, D>), dim3((uint32_t)((int64_t)n * n_heads)), dim3(256), 0, stream, A, unit)
   if (C.head_dim == 128) {
     if (unit == 64) { if (C.bf) M2C_ATTEND(true, 128, 64); else M2C_ATTEND(false, 128, 64); }
     else { if (C.bf) M2C_ATTEND(true, 128, 32); else M2C_ATTEND(false, 128, 32); }
