@@ -13,22 +13,37 @@ that on the stream of the call.
 """
 from __future__ import annotations
 
-import contextlib
-
 import torch
 
 from . import m2c
 
 _DTYPES = {torch.float16: m2c.DTYPE_FP16, torch.bfloat16: m2c.DTYPE_BF16}
+_I64x2 = m2c._I64x2
+_check = m2c._check
+# the address of a device's current stream without building a Stream object,
+# which takes as long as a launch
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on_stream(stream, device):
-    """Context in which torch allocates for `stream`."""
+def _raw(stream, device):
     if stream is None:
-        return contextlib.nullcontext()
+        return _current(device.index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _alloc(stream, device, *wanted):
+    """Tensors (shape, dtype) that torch's allocator keeps for `stream`."""
+    if stream is None:
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def _bad(msg):
@@ -37,14 +52,15 @@ def _bad(msg):
 
 def _rows(name, t, dtype, device, heads, dim):
     """Strides (tokens, heads) of rows [tokens][heads][dim]."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        _bad(f"{name}: shape {tuple(t.shape)}, need [tokens, {heads}, {dim}]")
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        _bad(f"{name}: shape {tuple(shape)}, need [tokens, {heads}, {dim}]")
     if t.dtype != dtype or t.device != device:
         _bad(f"{name}: {t.dtype} on {t.device}, need {dtype} on {device}")
     a, b, c = t.stride()
     if c != 1:
         _bad(f"{name}: the elements of a head must be contiguous")
-    return (a if t.shape[0] > 1 else dim, b if heads > 1 else 0)  # a single row's stride is free
+    return _I64x2(a if shape[0] > 1 else dim, b if heads > 1 else 0)  # a single row's stride is free
 
 
 def _ints(name, t, n, device):
@@ -70,29 +86,30 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
     if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
         _bad("q, k, v: need fp16 or bf16 GPU tensors [tokens, heads, head_dim]")
     dev, (tq, hq, d), hk = q.device, q.shape, k.shape[1]
-    desc = m2c.AttnDesc(_DTYPES[q.dtype], hq, hk, d, 1 if causal else 0, dev.index,
-                        0.0 if scale is None else scale, max_q)
     if v.shape != k.shape:
         _bad(f"v: shape {tuple(v.shape)}, k has {tuple(k.shape)}")
-    desc.q_stride = _rows("q", q, q.dtype, dev, hq, d)
-    desc.k_stride = _rows("k", k, q.dtype, dev, hk, d)
-    desc.v_stride = _rows("v", v, q.dtype, dev, hk, d)
     n = cu_q.shape[0] - 1 if cu_q.dim() == 1 else 0
     if n < 1:
         _bad("cu_q: need the row starts of at least one sequence and the end")
     _ints("cu_q", cu_q, n + 1, dev)
     cu_k = cu_q if cu_k is None else _ints("cu_k", cu_k, n + 1, dev)
+    strides = [_rows(name, t, q.dtype, dev, h, d) for name, t, h in (("q", q, hq), ("k", k, hk), ("v", v, hk))]
     lse = None
-    if out is None or return_lse:
-        with _on_stream(stream, dev):
-            if out is None:
-                out = torch.empty((tq, hq, d), dtype=q.dtype, device=dev)
-            if return_lse:
-                lse = torch.empty((tq, hq), dtype=torch.float32, device=dev)
-    if out.shape != q.shape:
-        _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
-    desc.out_stride = _rows("out", out, q.dtype, dev, hq, d)
-    m2c.m2c_prompt_attention(desc, q, k, v, cu_q, cu_k, n, tq, k.shape[0], out, lse, stream)
+    if out is not None:
+        if out.shape != q.shape:
+            _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+        if return_lse:
+            lse, = _alloc(stream, dev, ((tq, hq), torch.float32))
+    elif return_lse:
+        out, lse = _alloc(stream, dev, ((tq, hq, d), q.dtype), ((tq, hq), torch.float32))
+    else:
+        out, = _alloc(stream, dev, ((tq, hq, d), q.dtype))
+    desc = m2c.AttnDesc(_DTYPES[q.dtype], hq, hk, d, 1 if causal else 0, dev.index,
+                        0.0 if scale is None else scale, max_q, *strides,
+                        _rows("out", out, q.dtype, dev, hq, d))
+    _check(m2c.load().m2c_prompt_attention(
+        desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, tq,
+        k.shape[0], out.data_ptr(), _address(lse), _raw(stream, dev)))
     return (out, lse) if return_lse else out
 
 
@@ -138,6 +155,7 @@ class KVCache:
                     not t.is_contiguous():
                 _bad(f"{name}: need a contiguous {dt} tensor {shape} on {dev}")
             setattr(self, name, t)
+        self._lib, self._need = m2c.load(), {}  # _need: workspace bytes by call shape
         self.device, self.dtype = dev, dtype
         self.n_seqs, self.n_kv_heads, self.head_dim = n_seqs, n_kv_heads, head_dim
         self.max_blocks, self.block_tokens = max_blocks, block_tokens
@@ -155,7 +173,7 @@ class KVCache:
         """Forget the tokens of the listed sequences (default: all)."""
         n = self.n_seqs if seqs is None else seqs.shape[0]
         n, seqs = self._n(seqs, n)
-        m2c.m2c_kv_reset(self.desc, seqs, n, stream)
+        _check(self._lib.m2c_kv_reset(self.desc, _address(seqs), n, _raw(stream, self.device)))
 
     def append(self, k, v, cu=None, seqs=None, pos=None, stream=None):
         """Append rows of k and v [tokens, n_kv_heads, head_dim]: rows cu[b] ..
@@ -169,7 +187,9 @@ class KVCache:
         vs = _rows("v", v, self.dtype, self.device, self.n_kv_heads, self.head_dim)
         if v.shape[0] != k.shape[0]:
             _bad(f"v: {v.shape[0]} tokens, k has {k.shape[0]}")
-        m2c.m2c_kv_append(self.desc, seqs, n, cu, k.shape[0], pos, k, v, ks, vs, stream)
+        _check(self._lib.m2c_kv_append(self.desc, _address(seqs), n, _address(cu), k.shape[0],
+                                       _address(pos), k.data_ptr(), v.data_ptr(), ks, vs,
+                                       _raw(stream, self.device)))
 
     def read(self, cu, total=None, seqs=None, k=None, v=None, stream=None):
         """Tokens 0, 1, .. of sequence seqs[b] into rows cu[b] .. cu[b + 1] - 1
@@ -180,14 +200,14 @@ class KVCache:
         if (k is None) != (v is None) or (k is None) == (total is None):
             _bad("read: give k and v, or total")
         if k is None:
-            with _on_stream(stream, self.device):
-                k, v = (torch.empty((total, self.n_kv_heads, self.head_dim), dtype=self.dtype,
-                                    device=self.device) for _ in range(2))
+            rows = ((total, self.n_kv_heads, self.head_dim), self.dtype)
+            k, v = _alloc(stream, self.device, rows, rows)
         ks = _rows("k", k, self.dtype, self.device, self.n_kv_heads, self.head_dim)
         vs = _rows("v", v, self.dtype, self.device, self.n_kv_heads, self.head_dim)
         if v.shape[0] != k.shape[0]:
             _bad(f"v: {v.shape[0]} rows, k has {k.shape[0]}")
-        m2c.m2c_kv_read(self.desc, seqs, n, cu, k.shape[0], k, v, ks, vs, stream)
+        _check(self._lib.m2c_kv_read(self.desc, _address(seqs), n, cu.data_ptr(), k.shape[0],
+                                     k.data_ptr(), v.data_ptr(), ks, vs, _raw(stream, self.device)))
         return k, v
 
     def attend(self, q, seqs=None, max_len=0, scale=None, track=False, out=None, return_lse=False,
@@ -202,20 +222,29 @@ class KVCache:
         n, seqs = self._n(seqs, q.shape[0])
         qs = _rows("q", q, self.dtype, self.device, hq, self.head_dim)
         track = 1 if track else 0
-        need = m2c.m2c_kv_attend_workspace(self.desc, n, hq, track, max_len)
-        lse = work = None
-        with _on_stream(stream, self.device):
-            if out is None:
-                out = torch.empty((n, hq, self.head_dim), dtype=self.dtype, device=self.device)
-            if return_lse:
-                lse = torch.empty((n, hq), dtype=torch.float32, device=self.device)
-            if need:
-                work = torch.empty(need, dtype=torch.uint8, device=self.device)
-        if out.shape != q.shape:
+        key = (n, hq, track, max_len)
+        need = self._need.get(key)
+        if need is None:
+            if len(self._need) >= 4096:
+                self._need.clear()
+            need = self._need[key] = m2c.m2c_kv_attend_workspace(self.desc, *key)
+        want = []
+        if out is None:
+            want.append(((n, hq, self.head_dim), self.dtype))
+        elif out.shape != q.shape:
             _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+        if return_lse:
+            want.append(((n, hq), torch.float32))
+        if need:
+            want.append(((need,), torch.uint8))
+        got = iter(_alloc(stream, self.device, *want))
+        out = next(got) if out is None else out
+        lse = next(got) if return_lse else None
+        work = next(got) if need else None
         os = _rows("out", out, self.dtype, self.device, hq, self.head_dim)
-        m2c.m2c_kv_attend(self.desc, seqs, n, hq, 0.0 if scale is None else scale, q, qs, out, os,
-                          lse, track, max_len, work, need, stream)
+        _check(self._lib.m2c_kv_attend(self.desc, _address(seqs), n, hq, 0.0 if scale is None else scale,
+                                       q.data_ptr(), qs, out.data_ptr(), os, _address(lse), track,
+                                       max_len, _address(work), need, _raw(stream, self.device)))
         return (out, lse) if return_lse else out
 
     def evict(self, keep, first=0, recent=0, seqs=None, out=None, stream=None):
@@ -226,15 +255,15 @@ class KVCache:
         n, seqs = self._n(seqs, self.n_seqs if seqs is None else seqs.shape[0])
         to = (None, None, None)
         if out is not None:
-            to = tuple(out[name] for name in ("table", "weight", "len"))
-            for name, t in zip(("table", "weight", "len"), to):
-                own = getattr(self, name)
+            to = (out["table"], out["weight"], out["len"])
+            for name, t, own in zip(("table", "weight", "len"), to, (self.table, self.weight, self.len)):
                 if t.shape != own.shape or t.dtype != own.dtype or t.device != own.device or \
                         not t.is_contiguous():
                     _bad(f"out[{name!r}]: need a tensor like the cache's")
-        m2c.m2c_kv_evict(self.desc, seqs, n, keep, first, recent, *to, stream)
+        _check(self._lib.m2c_kv_evict(self.desc, _address(seqs), n, keep, first, recent,
+                                      *map(_address, to), _raw(stream, self.device)))
 
     def check(self, stream=None):
         """Wait for `stream`; raise what the calls so far found on the device
         (a sequence or page out of range, a full sequence, a bad place)."""
-        m2c.m2c_kv_status(self.desc, stream)
+        _check(self._lib.m2c_kv_status(self.desc, _raw(stream, self.device)))
