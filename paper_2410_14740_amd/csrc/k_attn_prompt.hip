@@ -216,17 +216,15 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
   const uint32_t ld_v = (uint32_t)(ld_row * A.v_tok) + ((lane % kChunks) ^ swz_v<D>(ld_row)) * 16;
   const uint32_t step_k = (uint32_t)(NW * kLoadRows * A.k_tok), step_v = (uint32_t)(NW * kLoadRows * A.v_tok);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds[0][0][0] + wave * 1024;
-  auto load_tile = [&](int t, int buf) {
+  auto load_tile = [&](const uint8_t* rows, int64_t tok, uint32_t off, uint32_t step, int t, uint32_t at) {
     const int left = min(kTileK, kl - t * kTileK) - 1;
-    const u32x4 bk = buffer_of(kb + (int64_t)t * kTileK * A.k_tok, (uint32_t)(left * A.k_tok) + kRowBytes);
-    const u32x4 bv = buffer_of(vb + (int64_t)t * kTileK * A.v_tok, (uint32_t)(left * A.v_tok) + kRowBytes);
-    const uint32_t dst = lds0 + buf * (2 * kTileBytes);
+    const u32x4 buf = buffer_of(rows + (int64_t)t * kTileK * tok, (uint32_t)(left * tok) + kRowBytes);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      load_lds16(bk, ld_k + i * step_k, dst + i * (NW * 1024));
-      load_lds16(bv, ld_v + i * step_v, dst + kTileBytes + i * (NW * 1024));
-    }
+    for (int i = 0; i < kLoads; ++i)
+      load_lds16(buf, off + i * step, lds0 + at + (t & 1) * (2 * kTileBytes) + i * (NW * 1024));
   };
+  auto load_k = [&](int t) { load_tile(kb, A.k_tok, ld_k, step_k, t, 0); };
+  auto load_v = [&](int t) { load_tile(vb, A.v_tok, ld_v, step_v, t, kTileBytes); };
 
   u32x4 qf[KS];
   {
@@ -255,11 +253,9 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
   float m = -INFINITY, l = 0.0f;
   uint32_t worst = 0;  // largest |value| bits seen in masked tiles, per half word
 
-  // One tile of keys. MASKED: some row of the wave misses some key of it.
-  auto compute = [&](int t, auto masked_t) {
-    constexpr bool MASKED = decltype(masked_t)::value;
-    const uint32_t buf = (t & 1) * (2 * kTileBytes), ka = k_lane + buf, va = v_lane + buf;
-    f32x16 s[2];
+  // S^T of tile t.
+  auto scores = [&](int t, f32x16 (&s)[2]) {
+    const uint32_t ka = k_lane + (t & 1) * (2 * kTileBytes);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -271,14 +267,13 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
       s[0] = mfma32<BF>(k_0, qf[ks], s[0]);
       s[1] = mfma32<BF>(k_1, qf[ks], s[1]);
     }
-    // four steps' keys ahead of the instructions that take them
-    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-    for (int ks = 0; ks < KS - 4; ++ks) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+  };
+  // Tile t from its scores s, and the scores of the next one into sn: those
+  // products do not wait for the softmax, and the softmax runs beside them.
+  // MASKED: some row of the wave misses some key of the tile.
+  auto compute = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2], auto masked_t) {
+    constexpr bool MASKED = decltype(masked_t)::value;
+    const uint32_t va = v_lane + (t & 1) * (2 * kTileBytes);
     if constexpr (MASKED) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -305,6 +300,7 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
     }
+    scores(t + 1, sn);
     const float base = (m == -INFINITY ? 0.0f : m) - kLift;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -315,12 +311,14 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
         sum[r & 3] += s[i][r];
       }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    u32x4 p[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      u32x4 p;
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        p[w] = pack16<BF>(s[u / 2][(u & 1) * 8 + 2 * w], s[u / 2][(u & 1) * 8 + 2 * w + 1]);
+        p[u][w] = pack16<BF>(s[u / 2][(u & 1) * 8 + 2 * w], s[u / 2][(u & 1) * 8 + 2 * w + 1]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const u32x2 lo = read_tr((va ^ (dt * 64)) + (16 * u) * kRowBytes);
@@ -335,30 +333,46 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
                                                     __builtin_bit_cast(us2, vf[w] & 0x7fff7fffu)));
           }
         }
-        o[dt] = mfma32<BF>(vf, p, o[dt]);
+        o[dt] = mfma32<BF>(vf, p[u], o[dt]);
       }
     }
   };
 
-  // Waves pass the barriers of the two loops together, each with its own number
-  // of tiles in the first.
-  if (nt > 0) load_tile(0, 0);
+  // Tile t needs V(t) and K(t + 1). Waves pass the barriers of the loops
+  // together, each with its own number of tiles in the first.
   const int plain = r0 >= ql ? 0 : wv_lo / kTileK;  // tiles that every row of the wave sees whole
   auto arrive = [&](int t) {
-    // this wave's part of tile t has landed and its reads of tile t - 1 are done
+    // this wave's loads have landed, and its reads of K(t) and V(t - 1) are done
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (t + 1 < nt) load_tile(t + 1, (t + 1) & 1);
+    if (t + 2 < nt) load_k(t + 2);
+    if (t + 1 < nt) load_v(t + 1);
   };
+  f32x16 s0[2], s1[2];
+  if (nt > 0) {
+    load_k(0);
+    load_v(0);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (nt > 1) load_k(1);
+    scores(0, s0);
+  }
   int t = 0;
-  for (; t < plain; ++t) {
+  for (; t + 1 < plain; t += 2) {
     arrive(t);
-    compute(t, std::false_type());
+    compute(t, s0, s1, std::false_type());
+    arrive(t + 1);
+    compute(t + 1, s1, s0, std::false_type());
   }
   for (; t < nt; ++t) {
     arrive(t);
-    if (t * kTileK < wv_hi) compute(t, std::true_type());
+    if (t * kTileK < wv_hi) {
+      compute(t, s0, s1, std::true_type());
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s0[i] = s1[i];
+    }
   }
   constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
   const bool bad = __ballot((worst & 0xffffu) >= kInf || (worst >> 16) >= kInf) != 0;
