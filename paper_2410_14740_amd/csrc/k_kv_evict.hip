@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(NT) evict_kernel(const KvView C, const int32_t
                                                    int first, int recent, int32_t* table_out,
                                                    float* weight_out, int32_t* len_out) {
   __shared__ uint32_t hist[256];
-  __shared__ uint32_t tmp[2][NT / 64];
+  __shared__ uint32_t tmp[3][NT / 64];
   const int b = blockIdx.x / C.n_kv_heads, head = blockIdx.x - b * C.n_kv_heads, tid = threadIdx.x;
   const int s = seqs ? seqs[b] : b;
   if (s < 0 || s >= C.n_seqs) {
@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(NT) evict_kernel(const KvView C, const int32_t
   const int lo = first, hi = m - recent;  // the blocks that compete
   uint32_t key = 0;
   int need = keep - first - recent;
+  bool all_ties = false;  // every block with that key is chosen
   if (need > 0) {
     for (int shift = 24; shift >= 0; shift -= 8) {
       for (int i = tid; i < 256; i += NT) hist[i] = 0;
@@ -94,11 +95,13 @@ __global__ void __launch_bounds__(NT) evict_kernel(const KvView C, const int32_t
       const int at = __ffsll((unsigned long long)__ballot(incl >= (uint32_t)need)) - 1;
       uint32_t above = incl - sum;
       int digit = 255 - 4 * l;
+      uint32_t count = d[0];
 #pragma unroll
       for (int i = 0; i < 3; ++i)
-        if (above + d[i] < (uint32_t)need && digit == 255 - 4 * l - i) above += d[i], --digit;
+        if (above + d[i] < (uint32_t)need && digit == 255 - 4 * l - i) above += d[i], --digit, count = d[i + 1];
       key = key << 8 | (uint32_t)__builtin_amdgcn_readlane(digit, at);
       need -= (int)__builtin_amdgcn_readlane((int)above, at);
+      all_ties = (int)__builtin_amdgcn_readlane((int)count, at) == need;
       __syncthreads();
     }
   }
@@ -106,16 +109,19 @@ __global__ void __launch_bounds__(NT) evict_kernel(const KvView C, const int32_t
   uint32_t ties = 0, kept_before = 0, gone_before = 0;
 #pragma unroll
   for (int j = 0; j < J; ++j) {
+    if (j * NT >= MB) break;
     const int e = j * NT + tid;
     const uint32_t k = score_key(w[j]);
     const bool mid = e >= lo && e < hi;
     const bool tie = mid && by_weight && k == key;
-    uint32_t total;
-    const uint32_t rank = ties + excl_scan<NT>(tie, tmp[0], &total);
-    ties += total;
+    uint32_t total, rank = 0;
+    if (!all_ties) {
+      rank = ties + excl_scan<NT>(tie, tmp[2], &total);
+      ties += total;
+    }
     const bool kept = e < m && (!mid || (by_weight && (k > key || (tie && rank < (uint32_t)need))));
     const bool out = e < m && !kept;
-    const uint32_t r = excl_scan<NT>((kept ? 1u : 0u) | (out ? 0x10000u : 0u), tmp[1], &total);
+    const uint32_t r = excl_scan<NT>((kept ? 1u : 0u) | (out ? 0x10000u : 0u), tmp[j & 1], &total);
     const int at = kept ? (int)(kept_before + (r & 0xffffu))
                    : out ? MB - gone + (int)(gone_before + (r >> 16)) : e - gone;
     kept_before += total & 0xffffu;
