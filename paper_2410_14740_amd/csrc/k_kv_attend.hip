@@ -121,11 +121,15 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   const bool known = s_id >= 0 && s_id < C.n_seqs;
   const int s = known ? s_id : 0;
   if (!known && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
+  const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
+  const int32_t* table = C.table + sh * C.max_blocks;
+  // The first chunk's pages, asked for before the length is known: lane i of a
+  // wave has its i-th unit's.
+  const int unit0 = split * A.chunk + wave + kWaves * lane;
+  int page0 = (unit0 >> halves) < C.max_blocks ? table[unit0 >> halves] : -1;
   const int len = known ? (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * BT) : 0;
   const int full = (len / BT) << halves;                  // units that lie in pages
   const int units = full + (len - len / BT * BT + UNIT - 1) / UNIT;
-  const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
-  const int32_t* table = C.table + sh * C.max_blocks;
   float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
                         : nullptr;
 
@@ -173,7 +177,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
     const int mine = u0 + wave + kWaves * lane;
     int page = 0;
     if (mine < min(u1, full)) {
-      page = table[mine >> halves];
+      page = mine == unit0 ? page0 : table[mine >> halves];
       if (page < 0 || page >= C.n_pages) {
         atomicOr(C.status, kKvBadIndex);
         page = -1;
