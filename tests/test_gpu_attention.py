@@ -182,6 +182,54 @@ def test_prompt_extreme_scores():
     check_prompt(q1, k1, v, lens, lens, True, out, lse, scale=1.0)
 
 
+def test_prompt_without_keys():
+    say("prompt without keys")
+    q, k = rand((5, 2, 64), F16, 34), rand((0, 2, 64), F16, 35)
+    for causal in (True, False):
+        out, lse = prompt_attention(q, k, k, starts([3, 2]), starts([0, 0]), causal=causal, return_lse=True)
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    assert prompt_attention(q[:0], k, k, starts([0, 0]), starts([0, 0])).shape == (0, 2, 64)
+
+
+def test_prompt_many_sequences():
+    """More sequences than a wave has lanes, empty ones among them."""
+    say("prompt many sequences")
+    ql = [(7 * i) % 150 if i % 5 else 0 for i in range(150)]
+    kl = [(11 * i) % 190 for i in range(150)]
+    q, k, v = rand((sum(ql), 2, 64), BF16, 36), rand((sum(kl), 1, 64), BF16, 37), rand((sum(kl), 1, 64), BF16, 38)
+    out, lse = prompt_attention(q, k, v, starts(ql), starts(kl), return_lse=True)
+    check_prompt(q, k, v, ql, kl, True, out, lse)
+    c = KVCache(150, 1, 64, 4, dtype=BF16)
+    shuffle_pages(c, 3)
+    c.append(k, v, cu=starts(kl))
+    check_cache(c, {b: (k[sum(kl[:b]):sum(kl[:b + 1])], v[sum(kl[:b]):sum(kl[:b + 1])]) for b in range(0, 150, 7)})
+    kk, _ = c.read(starts(kl), sum(kl))
+    assert float((kk.float() - k.float()).abs().max()) < 0.05
+    x = rand((150, 2, 64), BF16, 39)
+    o, e = c.attend(x, max_len=190, return_lse=True)
+    check_attend(c, x, o, e, list(range(150)))
+
+
+def test_prompt_offsets_past_32_bits():
+    """Head strides past 2^31 elements, and token strides whose sum passes them."""
+    say("prompt offsets past 32 bits")
+    buf = torch.empty(2 ** 31 + 2 ** 24, dtype=F16, device="cuda")
+    T, d = 100, 64
+    far = [(T, 2, d), (d, 2 ** 31, 1)]
+    x = rand((3, T, 2, d), F16, 44)
+    k, v = (buf.as_strided(*far, 2 * i * T * d) for i in range(2))
+    k.copy_(x[1]), v.copy_(x[2])
+    out = buf.as_strided(*far, 4 * T * d)
+    prompt_attention(x[0], k, v, starts([T]), out=out)
+    check_prompt(x[0], x[1], x[2], [T], [T], True, out, None)
+    wide = [(128, 1, d), (2 ** 24, d, 1)]
+    x = rand((3, 128, 1, d), F16, 45)
+    q, k, v = (buf.as_strided(*wide, i * d) for i in range(3))
+    for a, b in zip((q, k, v), x):
+        a.copy_(b)
+    check_prompt(*x, [128], [128], True, prompt_attention(q, k, v, starts([128])), None)
+
+
 @pytest.mark.parametrize("dt", [F16, BF16])
 def test_small_weights_beside_a_large_one(dt):
     """One key takes almost all the weight, thousands of others 2^-20 .. 2^-30
@@ -303,6 +351,37 @@ def test_append_in_pieces(dt, d, B):
         c.check()
         check_cache(c, {i: (k[i], v[i]) for i in range(n)})
         assert torch.equal(c.k_codes[c.table[5, :, :3].long()], whole.k_codes[whole.table[5, :, :3].long()])
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+def test_codes_of_every_significand(dt):
+    """Codes against an IEEE division for every significand of the block's
+    largest magnitude with every significand of an element, over the exponents
+    that give a code (keys: around 1; values: down among fp16's subnormals)."""
+    say(f"codes of every significand {dt}")
+    bits = 10 if dt == F16 else 7
+    n, B, D = 1 << bits, 128, 128
+    for top in (15, 10) if dt == F16 else (127, 20):  # exponent field of the largest
+        sig = torch.arange(n, dtype=torch.int32)
+        amax = (sig | top << bits)[:, None]
+        x = torch.cat([sig | (top - e) << bits for e in range(9)])[None].expand(n, -1)
+        x = torch.minimum(x, amax)
+        x = torch.nn.functional.pad(torch.cat([amax, x], 1), (0, -(9 * n + 1) % (B * D)))
+        x[:, 2::2] |= 0x8000  # half of them negative
+        blocks = x.reshape(-1, B * D)
+        if blocks.shape[0] > n:  # every block has its row's largest first
+            blocks[:, 0] = amax.expand(-1, blocks.shape[0] // n).reshape(-1)
+        vals = blocks.to(torch.int16).view(dt).view(-1, 1, D)
+        T = vals.shape[0]
+        c = KVCache(1, 1, D, T // B, block_tokens=B, dtype=dt)
+        c.append(vals.cuda(), vals.cuda(), cu=starts([T]))
+        c.check()
+        f = vals.float().view(-1, B * D)
+        s = f.abs().amax(1, keepdim=True).numpy() / np.float32(127)
+        want = np.rint(f.numpy() / s).astype(np.int8)
+        for codes, scale in ((c.k_codes, c.k_scale), (c.v_codes, c.v_scale)):
+            assert np.array_equal(scale.cpu().numpy(), s[:, 0])
+            assert np.array_equal(codes.view(-1, B * D).cpu().numpy(), want)
 
 
 def test_append_strides_seqs_and_places():
