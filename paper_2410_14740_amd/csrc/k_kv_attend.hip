@@ -495,8 +495,12 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   // the last round's end is ragged by less. (131071 tokens x 8 heads, 8 / 16 /
   // 32 / 48 units: 48, 45, 44, 53 us and a join of 20, 11, 6, 6; 32 sequences of
   // 500 .. 23254 tokens x 8 heads: 167, 150, 160, 200 us.)
+  // From 256 rows of up to 32 units on, a row is not split: the other half of
+  // the CU's waves would gain less than the join's launch takes (8 sequences of
+  // up to 2048 tokens x 32 heads: 17.4 us and a join of 4 against 18.4).
   int64_t chunk = (rows * units + 511) / 512;
   if (chunk > 32) chunk = 16;
+  else if (rows >= 256 && units <= 32) chunk = units;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
   while ((units + chunk - 1) / chunk > kMaxSplits) chunk += kWaves;
   S.chunk = (int)chunk;
