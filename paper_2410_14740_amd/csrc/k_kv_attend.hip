@@ -17,11 +17,19 @@
 // head's largest). So both products sum exact products in fp32, p alone is
 // rounded (fp16, relative 2^-12).
 //
-// A sequence is split into chunks of units; each workgroup's four waves take a
-// chunk's units in turn, each with its own running m, l, O, joined through LDS;
-// chunks are joined by a second launch where there are several.
+// The units of all rows (a row: a sequence, key/value head and tile of 16 query
+// heads), one after another, are cut into even shares, one per workgroup of a
+// grid that runs at once; the lengths are on the device, so each workgroup finds
+// its share itself. A share may end inside a row: the parts of a row are joined
+// by a second launch. Within a share the four waves take the units in turn, each
+// with its own running m, l, O, joined through LDS. Calls whose rows alone fill
+// the GPU, or with more sequences than a wave has lanes, give each workgroup a
+// chunk of one row instead.
+#include <algorithm>
+
 #include "ffn_device.h"
 #include "kv_device.h"
+#include "wave_ops.h"
 
 namespace m2c {
 
@@ -32,13 +40,13 @@ struct AttendArgs {
   uint8_t* out;
   float* lse;
   int64_t q_row, q_head, o_row, o_head;  // bytes
-  float* part_o;    // [n][n_heads][splits][D] unnormalized outputs of the splits
-  float2* part_ml;  // [n][n_heads][splits] their m and l
+  float* part_o;    // [parts of rows][min(group, 16)][D] unnormalized outputs
+  float2* part_ml;  // [parts of rows][min(group, 16)] their m and l
   float2* fin;      // [n][n_heads] m and 1 / l of the whole (track)
   float2* wsum;     // [n][n_kv_heads][units of max_blocks][group] m and sum of p by unit (track)
   float c;
   int n, n_heads, group, tiles;  // tiles: head tiles of 16 per key/value head
-  int splits, chunk;             // chunk: units per workgroup
+  int splits, chunk;             // chunk: units per workgroup (where shares are not even)
 };
 
 namespace {
@@ -96,7 +104,51 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t lo, uint32_t hi) {
   return __builtin_bit_cast(uint32_t, (half2v)(as_h2(u) - bias));
 }
 
-template <bool BF, int D, int UNIT>
+constexpr int kShares = 512;  // workgroups that run at once: two per CU
+
+// The even shares: lane b of a wave holds sequence b of the call, its rows' units
+// [start, start + cost * rows of a sequence) in the flat order.
+struct Shares {
+  int s, len;           // sequence id (-1: no such), tokens
+  uint32_t cost, start; // units of a row (at least 1), first flat unit
+  uint32_t total;
+  int count;            // shares: share p is units [p total / count, (p + 1) total / count)
+
+  __device__ __forceinline__ uint32_t first_of(int p) const {
+    return (uint32_t)((uint64_t)p * total / count);
+  }
+  __device__ __forceinline__ int owner_of(uint32_t f) const {
+    return (int)((((uint64_t)f + 1) * count - 1) / total);
+  }
+};
+
+__device__ __forceinline__ int units_of(int len, int BT, int unit) {
+  return len / BT * (BT / unit) + (len % BT + unit - 1) / unit;
+}
+
+__device__ __forceinline__ Shares shares_of(const AttendArgs& A, int unit) {
+  const KvView& C = A.C;
+  const int lane = threadIdx.x & 63, rows = C.n_kv_heads * A.tiles;
+  Shares S;
+  S.s = -1;
+  S.len = 0;
+  S.cost = 0;
+  if (lane < A.n) {
+    const int id = A.seqs ? A.seqs[lane] : lane;
+    if (id >= 0 && id < C.n_seqs) {
+      S.s = id;
+      S.len = (int)clamp64(C.len[id], 0, (int64_t)C.max_blocks * C.block_tokens);
+    }
+    S.cost = max(1, units_of(S.len, C.block_tokens, unit));
+  }
+  const uint32_t all = S.cost * rows, incl = wave_incl_scan(all);
+  S.start = incl - all;
+  S.total = __builtin_amdgcn_readlane(incl, 63);
+  S.count = min(kShares, max(A.n * rows, (int)(S.total / kWaves)));
+  return S;
+}
+
+template <bool BF, int D, int UNIT, bool EVEN>
 __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs A) {
   constexpr int T = UNIT / 16;   // token tiles of a unit
   constexpr int KS = D / 32;     // steps of the score product
@@ -110,30 +162,64 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   const KvView& C = A.C;
   const int lane = threadIdx.x & 63, col = lane & 15, qr = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = blockIdx.x / A.splits, split = blockIdx.x - row * A.splits;
-  const int ht = row % A.tiles, rk = row / A.tiles;
-  const int b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
-  const int heads = min(16, A.group - ht * 16);           // query heads of this tile
-  const int h0 = kvh * A.group + ht * 16;                 // the first
   const int BT = C.block_tokens;
   const int halves = BT / UNIT - 1;  // a block is one unit, or two: 0 or 1
-  const int s_id = A.seqs ? A.seqs[b] : b;
-  const bool known = s_id >= 0 && s_id < C.n_seqs;
-  const int s = known ? s_id : 0;
-  if (!known && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
+  Shares S;
+  uint32_t flat = 0, flat_end = 0;
+  if constexpr (EVEN) {
+    S = shares_of(A, UNIT);
+    if ((int)blockIdx.x >= S.count) return;
+    flat = S.first_of(blockIdx.x);
+    flat_end = S.first_of(blockIdx.x + 1);
+  }
+  do {  // the rows of a share
+  int b, rt, s_id, len, ua, ub, chunk, step, page0 = -1, unit0 = -1;
+  int64_t part;
+  bool whole;
+  if constexpr (EVEN) {
+    const int rows = C.n_kv_heads * A.tiles;
+    b = __ffsll((unsigned long long)__ballot(flat >= S.start && flat < S.start + S.cost * rows)) - 1;
+    const uint32_t cost = __builtin_amdgcn_readlane(S.cost, b);
+    const uint32_t at = flat - __builtin_amdgcn_readlane(S.start, b);
+    s_id = __builtin_amdgcn_readlane(S.s, b);
+    len = __builtin_amdgcn_readlane(S.len, b);
+    rt = (int)(at / cost);
+    ua = (int)(at - rt * cost);
+    const uint32_t take = min(cost - ua, flat_end - flat);
+    whole = take == cost;
+    ub = min(ua + (int)take, units_of(len, BT, UNIT));
+    chunk = step = 64 * kWaves;
+    part = (int64_t)b * rows + rt + blockIdx.x;  // a next row or a next share: one more
+    flat += take;
+  } else {
+    const int row = blockIdx.x / A.splits, split = blockIdx.x - row * A.splits;
+    const int rows = C.n_kv_heads * A.tiles;
+    b = row / rows, rt = row - b * rows;
+    s_id = A.seqs ? A.seqs[b] : b;
+    if (s_id < 0 || s_id >= C.n_seqs) s_id = -1;
+    // The first chunk's pages, asked for before the length is known: lane i of
+    // a wave has its i-th unit's.
+    unit0 = split * A.chunk + wave + kWaves * lane;
+    const int64_t at = ((int64_t)max(s_id, 0) * C.n_kv_heads + rt / A.tiles) * C.max_blocks;
+    page0 = (unit0 >> halves) < C.max_blocks ? C.table[at + (unit0 >> halves)] : -1;
+    len = s_id >= 0 ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * BT) : 0;
+    ua = split * A.chunk, ub = units_of(len, BT, UNIT);
+    chunk = A.chunk, step = A.splits * A.chunk;
+    part = blockIdx.x;
+    whole = A.splits == 1;
+    if (!whole && ua >= ub) return;  // a part without tokens; the join knows
+  }
+  if (s_id < 0 && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
+  const int s = max(s_id, 0);
+  const int kvh = rt / A.tiles, ht = rt - kvh * A.tiles, rk = b * C.n_kv_heads + kvh;
+  const int heads = min(16, A.group - ht * 16);           // query heads of this tile
+  const int h0 = kvh * A.group + ht * 16;                 // the first
   const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
   const int32_t* table = C.table + sh * C.max_blocks;
-  // The first chunk's pages, asked for before the length is known: lane i of a
-  // wave has its i-th unit's.
-  const int unit0 = split * A.chunk + wave + kWaves * lane;
-  int page0 = (unit0 >> halves) < C.max_blocks ? table[unit0 >> halves] : -1;
-  const int len = known ? (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * BT) : 0;
   const int full = (len / BT) << halves;                  // units that lie in pages
-  const int units = full + (len - len / BT * BT + UNIT - 1) / UNIT;
   float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
                         : nullptr;
 
-  if (A.splits > 1 && split * A.chunk >= units) return;  // a split without tokens; the join knows
   // queries: column = head, a step's elements where the key loads have them
   u32x4 qf[KS];
   const uint8_t* qrow = A.q + b * A.q_row + (h0 + min(col, heads - 1)) * A.q_head;
@@ -169,8 +255,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
 
-  for (int u0 = split * A.chunk; u0 < units; u0 += A.splits * A.chunk) {
-    const int u1 = min(units, u0 + A.chunk);
+  for (int u0 = ua; u0 < ub; u0 += step) {
+    const int u1 = min(ub, u0 + chunk);
     // A wave's units of the chunk are u0 + wave, + kWaves, .. (at most 64);
     // lane i holds the page of its i-th, -1 for one that does not exist: page 0
     // stands in with scales of 0, a block of zeros.
@@ -368,68 +454,87 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
       *(f32x4*)&mrg[wave][col][(qr * 4 + r) * E + i] = f32x4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]};
   __syncthreads();
   const int hd = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * E;
-  if (hd >= heads) return;
-  float M = -INFINITY, L = 0.0f, fac[kWaves];
+  if (hd < heads) {
+    float M = -INFINITY, L = 0.0f, fac[kWaves];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mls[w][hd].x);
-  const float mu = M == -INFINITY ? 0.0f : M;
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mls[w][hd].x);
+    const float mu = M == -INFINITY ? 0.0f : M;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    fac[w] = exp2_fast(mls[w][hd].x - mu);
-    L += mls[w][hd].y * fac[w];
+    for (int w = 0; w < kWaves; ++w) {
+      fac[w] = exp2_fast(mls[w][hd].x - mu);
+      L += mls[w][hd].y * fac[w];
+    }
+    float y[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) y[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = fmaf(mrg[w][hd][d0 + i], fac[w], y[i]);
+    if (whole) {
+      const int64_t at = (int64_t)b * A.n_heads + h0 + hd;
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      uint32_t* po = (uint32_t*)(A.out + b * A.o_row + (h0 + hd) * A.o_head + d0 * 2);
+#pragma unroll
+      for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
+      if ((threadIdx.x & 15) == 0) {
+        if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
+        if (A.fin) A.fin[at] = make_float2(M, inv);
+      }
+    } else {
+      const int64_t at = part * min(A.group, 16) + hd;
+      if ((threadIdx.x & 15) == 0) A.part_ml[at] = make_float2(M, L);
+      float* po = A.part_o + at * D + d0;
+#pragma unroll
+      for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+    }
   }
-  float y[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) y[i] = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = fmaf(mrg[w][hd][d0 + i], fac[w], y[i]);
-  const int64_t at = (int64_t)b * A.n_heads + h0 + hd;
-  if (A.splits > 1) {
-    if ((threadIdx.x & 15) == 0) A.part_ml[at * A.splits + split] = make_float2(M, L);
-    float* po = A.part_o + (at * A.splits + split) * D + d0;
-#pragma unroll
-    for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
-    return;
-  }
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  uint32_t* po = (uint32_t*)(A.out + b * A.o_row + (h0 + hd) * A.o_head + d0 * 2);
-#pragma unroll
-  for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
-  if ((threadIdx.x & 15) == 0) {
-    if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
-    if (A.fin) A.fin[at] = make_float2(M, inv);
-  }
+  if (EVEN) __syncthreads();  // the next row writes the same LDS
+  } while (EVEN && flat < flat_end);
 }
 
-// Joins the splits of one query head: 256 threads, D / 4 of them per split.
-template <bool BF, int D>
+// Joins the parts of one query head's row: 256 threads, D / 4 of them per part.
+template <bool BF, int D, bool EVEN>
 __global__ void __launch_bounds__(256) join_kernel(const AttendArgs A, int unit) {
   constexpr int TS = D / 4, GR = 256 / TS;
   __shared__ __align__(16) f32x4 acc[GR][TS];
-  const int tid = threadIdx.x;
-  const int64_t at = blockIdx.x;
-  const int b = (int)(at / A.n_heads), h = (int)(at - (int64_t)b * A.n_heads);
-  const int s_id = A.seqs ? A.seqs[b] : b;
   const KvView& C = A.C;
-  const int len = s_id >= 0 && s_id < C.n_seqs
-                      ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * C.block_tokens) : 0;
-  const int used = min(A.splits, (len + A.chunk * unit - 1) / (A.chunk * unit));  // splits with tokens
-  const float2* ml = A.part_ml + at * A.splits;
+  const int tid = threadIdx.x;
+  const int b = blockIdx.x / A.n_heads, h = blockIdx.x - b * A.n_heads;
+  const int rows = C.n_kv_heads * A.tiles, th = min(A.group, 16);
+  const int kvh = h / A.group, hg = h - kvh * A.group, rt = kvh * A.tiles + hg / 16, hd = hg % 16;
+  int64_t first;
+  int parts;
+  if constexpr (EVEN) {
+    const Shares S = shares_of(A, unit);
+    const uint32_t cost = __builtin_amdgcn_readlane(S.cost, b);
+    const uint32_t at = __builtin_amdgcn_readlane(S.start, b) + rt * cost;
+    const int p = S.owner_of(at);
+    parts = S.owner_of(at + cost - 1) - p + 1;
+    if (parts == 1) return;  // its workgroup had all of it
+    first = (int64_t)b * rows + rt + p;
+  } else {
+    const int s_id = A.seqs ? A.seqs[b] : b;
+    const int len = s_id >= 0 && s_id < C.n_seqs
+                        ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * C.block_tokens) : 0;
+    const int units = units_of(len, C.block_tokens, unit);
+    parts = min(A.splits, (units + A.chunk - 1) / A.chunk);  // those with tokens
+    first = ((int64_t)b * rows + rt) * A.splits;
+  }
+  const float2* ml = A.part_ml + first * th + hd;
   float M = -INFINITY, L = 0.0f;
-  for (int s = tid & 63; s < used; s += 64) M = fmaxf(M, ml[s].x);
+  for (int s = tid & 63; s < parts; s += 64) M = fmaxf(M, ml[s * th].x);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
   const float mu = M == -INFINITY ? 0.0f : M;
-  for (int s = tid & 63; s < used; s += 64) L += ml[s].y * exp2_fast(ml[s].x - mu);
+  for (int s = tid & 63; s < parts; s += 64) L += ml[s * th].y * exp2_fast(ml[s * th].x - mu);
   L = wave_sum(L);
   f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-  const float* po = A.part_o + at * A.splits * D + (tid % TS) * 4;
+  const float* po = A.part_o + (first * th + hd) * D + (tid % TS) * 4;
 #pragma unroll 4
-  for (int s = tid / TS; s < used; s += GR) {
-    const float f = exp2_fast(ml[s].x - mu);
-    const f32x4 v = *(const f32x4*)(po + (int64_t)s * D);
+  for (int s = tid / TS; s < parts; s += GR) {
+    const float f = exp2_fast(ml[s * th].x - mu);
+    const f32x4 v = *(const f32x4*)(po + (int64_t)s * th * D);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = fmaf(v[i], f, y[i]);
   }
@@ -441,6 +546,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs A, int unit)
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] += acc[g][tid][i];
   const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  const int64_t at = blockIdx.x;
   uint32_t* out = (uint32_t*)(A.out + b * A.o_row + h * A.o_head + tid * 8);
   out[0] = pack16<BF>(y[0] * inv, y[1] * inv);
   out[1] = pack16<BF>(y[2] * inv, y[3] * inv);
@@ -480,6 +586,8 @@ constexpr int kMaxSplits = 1024;
 
 struct Split {
   int tiles, splits, chunk;
+  bool even;
+  int64_t parts;  // of rows, that the join reads
 };
 
 Split split_of(const KvView& C, int n, int n_heads, int max_len) {
@@ -490,15 +598,13 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   Split S;
   S.tiles = (group + 15) / 16;
   const int64_t rows = (int64_t)n * C.n_kv_heads * S.tiles;
-  // 512 workgroups run at once (two per CU). Up to 32 units each, one round of
-  // them covers the call; more come in rounds of 16 units, shorter ones, so that
-  // the last round's end is ragged by less. (131071 tokens x 8 heads, 8 / 16 /
-  // 32 / 48 units: 48, 45, 44, 53 us and a join of 20, 11, 6, 6; 32 sequences of
-  // 500 .. 23254 tokens x 8 heads: 167, 150, 160, 200 us.)
-  // From 256 rows of up to 32 units on, a row is not split: the other half of
-  // the CU's waves would gain less than the join's launch takes (8 sequences of
-  // up to 2048 tokens x 32 heads: 17.4 us and a join of 4 against 18.4).
-  int64_t chunk = (rows * units + 511) / 512;
+  // A row is left whole where it is four units, or where 256 rows of up to 32
+  // units are enough workgroups: the other half of the CU's waves would gain
+  // less than the join's launch takes (8 sequences of up to 2048 tokens x 32
+  // heads: 17.4 us and a join of 4 against 18.4). Else the shares are even where
+  // a wave can hold the sequences, and chunks of up to 32 units (16 where that
+  // is more than a round of workgroups) where there are more.
+  int64_t chunk = (rows * units + kShares - 1) / kShares;
   if (chunk > 32) chunk = 16;
   else if (rows >= 256 && units <= 32) chunk = units;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
@@ -506,6 +612,8 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   S.chunk = (int)chunk;
   S.splits = (int)((units + chunk - 1) / chunk);
   if (S.splits < 1) S.splits = 1;
+  S.even = S.splits > 1 && n <= 64 && rows * (cap / unit) < INT32_MAX;
+  S.parts = S.splits == 1 ? 0 : S.even ? rows + kShares : rows * S.splits;
   return S;
 }
 
@@ -516,9 +624,8 @@ int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t kv_attend_workspace(const KvView& C, int n, int n_heads, int track, int max_len) {
   const Split S = split_of(C, n, n_heads, max_len);
   int64_t bytes = 0;
-  if (S.splits > 1)
-    bytes += round256((int64_t)n * n_heads * S.splits * 8) +
-             round256((int64_t)n * n_heads * S.splits * C.head_dim * 4);
+  const int64_t part_heads = S.parts * std::min(n_heads / C.n_kv_heads, 16);
+  if (S.parts) bytes += round256(part_heads * 8) + round256(part_heads * C.head_dim * 4);
   if (track)
     bytes += round256((int64_t)n * n_heads * 8) +
              round256((int64_t)n * n_heads * C.max_blocks * (C.block_tokens / unit_of(C)) * 8);
@@ -545,11 +652,12 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
   A.splits = S.splits;
   A.chunk = S.chunk;
   uint8_t* ws = (uint8_t*)workspace;
-  if (S.splits > 1) {
+  const int64_t part_heads = S.parts * std::min(A.group, 16);
+  if (S.parts) {
     A.part_ml = (float2*)ws;
-    ws += round256((int64_t)n * n_heads * S.splits * 8);
+    ws += round256(part_heads * 8);
     A.part_o = (float*)ws;
-    ws += round256((int64_t)n * n_heads * S.splits * C.head_dim * 4);
+    ws += round256(part_heads * C.head_dim * 4);
   }
   if (track) {
     A.fin = (float2*)ws;
@@ -557,27 +665,32 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
     A.wsum = (float2*)ws;
   }
   const int unit = unit_of(C);
-  const int64_t grid = (int64_t)n * C.n_kv_heads * S.tiles * S.splits;
+  const int64_t grid = S.even ? kShares : (int64_t)n * C.n_kv_heads * S.tiles * S.splits;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-#define M2C_ATTEND(BF, D, U) \
-  hipLaunchKernelGGL((attend_kernel<BF, D, U>), dim3((uint32_t)grid), dim3(kWaves * 64), 0, stream, A)
-#define M2C_JOIN(BF, D) \
-  hipLaunchKernelGGL((join_kernel<BF, D>), dim3((uint32_t)((int64_t)n * n_heads)), dim3(256), 0, stream, A, unit)
-  if (C.head_dim == 128) {
-    if (unit == 64) { if (C.bf) M2C_ATTEND(true, 128, 64); else M2C_ATTEND(false, 128, 64); }
-    else { if (C.bf) M2C_ATTEND(true, 128, 32); else M2C_ATTEND(false, 128, 32); }
-  } else {
-    if (unit == 64) { if (C.bf) M2C_ATTEND(true, 64, 64); else M2C_ATTEND(false, 64, 64); }
-    else { if (C.bf) M2C_ATTEND(true, 64, 32); else M2C_ATTEND(false, 64, 32); }
-  }
-  hipError_t e = hipGetLastError();
+  const auto launch = [&](auto bf, auto d, auto u, auto even) {
+    constexpr bool BF = decltype(bf)::value, EVEN = decltype(even)::value;
+    constexpr int D = decltype(d)::value, UNIT = decltype(u)::value;
+    hipLaunchKernelGGL((attend_kernel<BF, D, UNIT, EVEN>), dim3((uint32_t)grid), dim3(kWaves * 64), 0,
+                       stream, A);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !S.parts) return e;
+    hipLaunchKernelGGL((join_kernel<BF, D, EVEN>), dim3((uint32_t)(n * n_heads)), dim3(256), 0, stream,
+                       A, UNIT);
+    return hipGetLastError();
+  };
+  const auto by_even = [&](auto bf, auto d, auto u) {
+    return S.even ? launch(bf, d, u, std::true_type()) : launch(bf, d, u, std::false_type());
+  };
+  const auto by_unit = [&](auto bf, auto d) {
+    return unit == 64 ? by_even(bf, d, std::integral_constant<int, 64>())
+                      : by_even(bf, d, std::integral_constant<int, 32>());
+  };
+  const auto by_dim = [&](auto bf) {
+    return C.head_dim == 128 ? by_unit(bf, std::integral_constant<int, 128>())
+                             : by_unit(bf, std::integral_constant<int, 64>());
+  };
+  hipError_t e = C.bf ? by_dim(std::true_type()) : by_dim(std::false_type());
   if (e != hipSuccess) return e;
-  if (S.splits > 1) {
-    if (C.head_dim == 128) { if (C.bf) M2C_JOIN(true, 128); else M2C_JOIN(false, 128); }
-    else { if (C.bf) M2C_JOIN(true, 64); else M2C_JOIN(false, 64); }
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   if (track) {
     const int64_t cap = (int64_t)C.max_blocks * C.block_tokens;
     const int64_t most = max_len > 0 && max_len < cap ? max_len : cap;
@@ -588,8 +701,6 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
                        A, unit, parts);
     e = hipGetLastError();
   }
-#undef M2C_ATTEND
-#undef M2C_JOIN
   return e;
 }
 

@@ -610,6 +610,23 @@ def test_attend(hq, hk, d, B, dt, lens):
     check_attend(c, q, o, None, seqs, before=before)
 
 
+@pytest.mark.parametrize("n", [64, 70])
+def test_attend_many_ragged_sequences(n):
+    """As many sequences as a wave has lanes, and more; the longest split, some empty, heads over two tiles."""
+    say(f"attend {n} ragged sequences")
+    lens = [(37 * i) % 400 if i % 6 else 0 for i in range(n)]
+    lens[n // 2], lens[-1] = 3000, 1500
+    c = filled(lens, 1, 64, 32, F16, 100, 115)
+    q = rand((n, 20, 64), F16, 118, 1.5)
+    before = c.weight.clone()
+    out, lse = c.attend(q, max_len=3000, track=True, return_lse=True)
+    c.check()
+    check_attend(c, q, out, lse, list(range(n)), before=before)
+    for hint in (0, 64, 500):
+        o, e = c.attend(q, max_len=hint, return_lse=True)
+        check_attend(c, q, o, e, list(range(n)))
+
+
 def test_attend_rows_strides_and_scale():
     say("attend subset, strides, scale")
     c = filled([70, 0, 500, 64, 129], 2, 128, 64, BF16, 9, 120)
