@@ -2,7 +2,9 @@
 // and key/value head a selection of the heaviest blocks (ties to the lowest
 // index) and one ordered move of the head's table and weight rows. 16 bytes per
 // table entry and no page data: latency-bound, one workgroup per row with the
-// row in registers.
+// row in registers. Measured: 256 rows of 34 entries 4.0 us, of 2049 entries
+// 8.2 us (8.4 MB), a third of it four passes of a histogram with three barriers
+// each. (The first pass's adds made one per digit and wave by ballots: 9.3 us.)
 #include "kv_device.h"
 #include "wave_ops.h"
 
