@@ -498,9 +498,21 @@ typedef struct {
   int32_t device;        /* HIP device ordinal of every pointer                 */
   float scale;           /* factor of <q, k>; 0 = 1 / sqrt(head_dim)            */
   int32_t max_q;         /* longest query sequence, or 0 if not known: only
-                            chooses the kernel's tile, never what is computed   */
+                            helps to choose whether rows are split along their
+                            keys, never what is computed                        */
   int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2]; /* token, head  */
+  void* workspace;       /* dev, 256-byte aligned, not shared with a call that
+                            may run at the same time, or NULL: no row of
+                            queries is then split along its keys                */
+  int64_t workspace_bytes;
 } m2c_attn_desc;
+
+/* Bytes of the workspace with which a call with these arguments splits the
+ * queries that see many more keys than the others along them (0 where it would
+ * split none), or -1. cu_q and cu_k are compared, not read. */
+int64_t m2c_prompt_attention_workspace(const m2c_attn_desc* desc, const int32_t* cu_q,
+                                       const int32_t* cu_k, int32_t n_seqs, int64_t total_q,
+                                       int64_t total_k);
 
 /* Attention of packed sequences: rows cu_q[b] .. cu_q[b + 1] - 1 of q and out
  * and rows cu_k[b] .. cu_k[b + 1] - 1 of k and v are sequence b.
@@ -509,7 +521,7 @@ typedef struct {
  *   q, out      dev [total_q] rows;  k, v  dev [total_k] rows
  *   lse         dev fp32 [total_q][n_heads], ln sum exp(scale <q, k>), or NULL
  * Output rows of no sequence are not written. Results are the same bits on
- * every run. */
+ * every run with the same arguments. */
 m2c_status m2c_prompt_attention(const m2c_attn_desc* desc, const void* q, const void* k,
                                 const void* v, const int32_t* cu_q, const int32_t* cu_k,
                                 int32_t n_seqs, int64_t total_q, int64_t total_k, void* out,

@@ -72,6 +72,9 @@ def _ints(name, t, n, device):
     return t
 
 
+_prompt_need = {}  # workspace bytes by call shape
+
+
 def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None, out=None,
                      return_lse=False, stream=None):
     """Attention of packed prompts.
@@ -80,7 +83,8 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
     bf16, any token and head strides that are multiples of 8 elements (rows of
     a fused projection, for example). cu_q, cu_k: int32 [sequences + 1] row
     starts (cu_k None: the same). causal: query i of lq sees keys 0 .. lk - lq
-    + i of its sequence. max_q: longest query sequence if known (a hint).
+    + i of its sequence. max_q: longest query sequence if known (a hint
+    for whether rows are split along their keys).
     Returns out like q (contiguous unless given), or (out, lse) with lse fp32
     [total_q, n_heads] = ln sum exp(scale q.k)."""
     if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
@@ -94,19 +98,30 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
     _ints("cu_q", cu_q, n + 1, dev)
     cu_k = cu_q if cu_k is None else _ints("cu_k", cu_k, n + 1, dev)
     strides = [_rows(name, t, q.dtype, dev, h, d) for name, t, h in (("q", q, hq), ("k", k, hk), ("v", v, hk))]
-    lse = None
-    if out is not None:
-        if out.shape != q.shape:
-            _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
-        if return_lse:
-            lse, = _alloc(stream, dev, ((tq, hq), torch.float32))
-    elif return_lse:
-        out, lse = _alloc(stream, dev, ((tq, hq, d), q.dtype), ((tq, hq), torch.float32))
-    else:
-        out, = _alloc(stream, dev, ((tq, hq, d), q.dtype))
+    if out is not None and out.shape != q.shape:
+        _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
     desc = m2c.AttnDesc(_DTYPES[q.dtype], hq, hk, d, 1 if causal else 0, dev.index,
-                        0.0 if scale is None else scale, max_q, *strides,
-                        _rows("out", out, q.dtype, dev, hq, d))
+                        0.0 if scale is None else scale, max_q, *strides)
+    key = (hq, hk, d, n, tq, k.shape[0], max_q, cu_q.data_ptr() == cu_k.data_ptr())
+    need = _prompt_need.get(key)
+    if need is None:
+        if len(_prompt_need) >= 4096:
+            _prompt_need.clear()
+        need = _prompt_need[key] = m2c.m2c_prompt_attention_workspace(desc, cu_q, cu_k, n, tq, k.shape[0])
+    want = []
+    if out is None:
+        want.append(((tq, hq, d), q.dtype))
+    if return_lse:
+        want.append(((tq, hq), torch.float32))
+    if need:
+        want.append(((need,), torch.uint8))
+    got = iter(_alloc(stream, dev, *want))
+    out = next(got) if out is None else out
+    lse = next(got) if return_lse else None
+    if need:
+        work = next(got)
+        desc.workspace, desc.workspace_bytes = work.data_ptr(), need
+    desc.out_stride = _rows("out", out, q.dtype, dev, hq, d)
     _check(m2c.load().m2c_prompt_attention(
         desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, tq,
         k.shape[0], out.data_ptr(), _address(lse), _raw(stream, dev)))
@@ -121,7 +136,7 @@ class KVCache:
     of m2c_kv_cache as attributes of the same names: k_codes, v_codes, k_scale,
     v_scale, tail_k, tail_v, table, len, weight, arrive, status. `n_pages`
     defaults to one page for every table entry, and `table` to those in order;
-    with fewer pages the caller sets table entries before blocks fill."""
+    with fewer pages it is -1 and the caller sets entries before blocks fill."""
 
     def __init__(self, n_seqs, n_kv_heads, head_dim, max_blocks, block_tokens=64,
                  dtype=torch.float16, n_pages=None, device=None, tensors=None):
@@ -150,7 +165,8 @@ class KVCache:
                 make = torch.empty if name in ("k_codes", "v_codes", "tail_k", "tail_v") else torch.zeros
                 t = make(shape, dtype=dt, device=dev)
                 if name == "table":
-                    t = torch.arange(entries, dtype=torch.int32, device=dev).remainder_(n_pages).view(shape)
+                    t = torch.arange(entries, dtype=torch.int32, device=dev).view(shape) if n_pages >= entries \
+                        else t.fill_(-1)
             if t is None or tuple(t.shape) != shape or t.dtype != dt or t.device != dev or \
                     not t.is_contiguous():
                 _bad(f"{name}: need a contiguous {dt} tensor {shape} on {dev}")

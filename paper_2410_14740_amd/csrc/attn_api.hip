@@ -2,6 +2,7 @@
 #include "kv_device.h"
 
 namespace m2c {
+int64_t prompt_workspace(const m2c_attn_desc* D, bool self, int n_seqs, int64_t total_q, int64_t total_k);
 hipError_t launch_prompt_attention(const m2c_attn_desc* D, const void* q, const void* k,
                                    const void* v, const int32_t* cu_q, const int32_t* cu_k,
                                    int n_seqs, int64_t total_q, int64_t total_k, void* out,
@@ -98,10 +99,24 @@ m2c_status view_of(const m2c_kv_cache* c, KvView* v) {
   return M2C_OK;
 }
 
-m2c_status check_n(const KvView& C, const int32_t* seqs, int n) {
+m2c_status check_n(const KvView& C, int n) {
   if (n < 1 || n > C.n_seqs)
     return api_fail(M2C_ERR_INVALID_ARG, "n %d: need [1, n_seqs=%d]", n, C.n_seqs);
-  (void)seqs;
+  return M2C_OK;
+}
+
+m2c_status check_prompt(const m2c_attn_desc* D, int n_seqs, int64_t total_q, int64_t total_k) {
+  if (!D) return api_fail(M2C_ERR_INVALID_ARG, "prompt attention: NULL argument");
+  const m2c_status rc = check_heads(D->dtype, D->n_heads, D->n_kv_heads, D->head_dim, D->scale, D->device);
+  if (rc != M2C_OK) return rc;
+  if (D->causal != 0 && D->causal != 1)
+    return api_fail(M2C_ERR_INVALID_ARG, "causal %d: need 0 or 1", D->causal);
+  if (D->max_q < 0) return api_fail(M2C_ERR_INVALID_ARG, "max_q %d: need >= 0", D->max_q);
+  if (n_seqs < 1 || n_seqs > 65535)
+    return api_fail(M2C_ERR_INVALID_ARG, "n_seqs %d: need [1, 65535]", n_seqs);
+  if (total_q < 0 || total_q > kMaxRows || total_k < 0 || total_k > kMaxRows)
+    return api_fail(M2C_ERR_INVALID_ARG, "total_q %lld, total_k %lld: need [0, 2^30]",
+                    (long long)total_q, (long long)total_k);
   return M2C_OK;
 }
 
@@ -115,20 +130,27 @@ m2c_status check_n(const KvView& C, const int32_t* seqs, int n) {
 
 extern "C" {
 
+int64_t m2c_prompt_attention_workspace(const m2c_attn_desc* D, const int32_t* cu_q, const int32_t* cu_k,
+                                       int32_t n_seqs, int64_t total_q, int64_t total_k) {
+  if (check_prompt(D, n_seqs, total_q, total_k) != M2C_OK) return -1;
+  return total_q ? m2c::prompt_workspace(D, cu_q == cu_k, n_seqs, total_q, total_k) : 0;
+}
+
 m2c_status m2c_prompt_attention(const m2c_attn_desc* D, const void* q, const void* k, const void* v,
                                 const int32_t* cu_q, const int32_t* cu_k, int32_t n_seqs,
                                 int64_t total_q, int64_t total_k, void* out, float* lse,
                                 void* stream) {
-  if (!D || !cu_q || !cu_k) return api_fail(M2C_ERR_INVALID_ARG, "prompt attention: NULL argument");
-  CHECKED(check_heads(D->dtype, D->n_heads, D->n_kv_heads, D->head_dim, D->scale, D->device));
-  if (D->causal != 0 && D->causal != 1)
-    return api_fail(M2C_ERR_INVALID_ARG, "causal %d: need 0 or 1", D->causal);
-  if (n_seqs < 1 || n_seqs > 65535)
-    return api_fail(M2C_ERR_INVALID_ARG, "n_seqs %d: need [1, 65535]", n_seqs);
-  if (total_q < 0 || total_q > kMaxRows || total_k < 0 || total_k > kMaxRows)
-    return api_fail(M2C_ERR_INVALID_ARG, "total_q %lld, total_k %lld: need [0, 2^30]",
-                    (long long)total_q, (long long)total_k);
+  CHECKED(check_prompt(D, n_seqs, total_q, total_k));
+  if (!cu_q || !cu_k) return api_fail(M2C_ERR_INVALID_ARG, "prompt attention: NULL argument");
   if (total_q == 0) return M2C_OK;
+  if (D->workspace) {
+    const int64_t need = m2c::prompt_workspace(D, cu_q == cu_k, n_seqs, total_q, total_k);
+    if ((uintptr_t)D->workspace & 255)
+      return api_fail(M2C_ERR_INVALID_ARG, "workspace: not 256-byte aligned");
+    if (D->workspace_bytes < need)
+      return api_fail(M2C_ERR_CAPACITY, "workspace of %lld bytes: need %lld", (long long)D->workspace_bytes,
+                      (long long)need);
+  }
   CHECKED(check_rows("q", q, D->q_stride, D->head_dim));
   CHECKED(check_rows("out", out, D->out_stride, D->head_dim));
   if (total_k > 0) {
@@ -145,7 +167,7 @@ m2c_status m2c_prompt_attention(const m2c_attn_desc* D, const void* q, const voi
 m2c_status m2c_kv_reset(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream) {
   KvView C;
   CHECKED(view_of(cache, &C));
-  CHECKED(check_n(C, seqs, n));
+  CHECKED(check_n(C, n));
   CurrentDevice g(cache->device);
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_reset(C, seqs, n, (hipStream_t)stream), "reset");
@@ -157,7 +179,7 @@ m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
                          void* stream) {
   KvView C;
   CHECKED(view_of(cache, &C));
-  CHECKED(check_n(C, seqs, n));
+  CHECKED(check_n(C, n));
   if (total < 0 || total > kMaxRows || (!cu && total != n))
     return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30], and n without cu", (long long)total);
   if (total == 0) return M2C_OK;
@@ -174,7 +196,7 @@ m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n
                        const int64_t v_stride[2], void* stream) {
   KvView C;
   CHECKED(view_of(cache, &C));
-  CHECKED(check_n(C, seqs, n));
+  CHECKED(check_n(C, n));
   if (!cu) return api_fail(M2C_ERR_INVALID_ARG, "cu is NULL");
   if (total < 0 || total > kMaxRows)
     return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30]", (long long)total);
@@ -190,9 +212,13 @@ m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n
 int64_t m2c_kv_attend_workspace(const m2c_kv_cache* cache, int32_t n, int32_t n_heads, int32_t track,
                                 int32_t max_len) {
   KvView C;
-  if (view_of(cache, &C) != M2C_OK || check_n(C, nullptr, n) != M2C_OK ||
+  if (view_of(cache, &C) != M2C_OK || check_n(C, n) != M2C_OK ||
       check_heads(cache->dtype, n_heads, C.n_kv_heads, C.head_dim, 0.0f, cache->device) != M2C_OK)
     return -1;
+  if (max_len < 0) {
+    api_fail(M2C_ERR_INVALID_ARG, "max_len %d: need >= 0", max_len);
+    return -1;
+  }
   return m2c::kv_attend_workspace(C, n, n_heads, track != 0, max_len);
 }
 
@@ -202,7 +228,7 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
                          void* workspace, int64_t workspace_bytes, void* stream) {
   KvView C;
   CHECKED(view_of(cache, &C));
-  CHECKED(check_n(C, seqs, n));
+  CHECKED(check_n(C, n));
   CHECKED(check_heads(cache->dtype, n_heads, C.n_kv_heads, C.head_dim, scale, cache->device));
   if (track != 0 && track != 1) return api_fail(M2C_ERR_INVALID_ARG, "track %d: need 0 or 1", track);
   if (max_len < 0) return api_fail(M2C_ERR_INVALID_ARG, "max_len %d: need >= 0", max_len);
@@ -225,7 +251,7 @@ m2c_status m2c_kv_evict(const m2c_kv_cache* cache, const int32_t* seqs, int32_t 
                         int32_t* len_out, void* stream) {
   KvView C;
   CHECKED(view_of(cache, &C));
-  CHECKED(check_n(C, seqs, n));
+  CHECKED(check_n(C, n));
   if (first < 0 || recent < 0 || keep < 0 || (int64_t)first + recent > keep)
     return api_fail(M2C_ERR_INVALID_ARG, "keep %d, first %d, recent %d: need first + recent <= keep",
                     keep, first, recent);

@@ -90,21 +90,21 @@ __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) {
 }
 
 // The work items of packed sequences in one flat range without a prefix sum:
-// sequence b owns items item_start(cu[b], b) .. item_start(cu[b + 1], b + 1) - 1,
-// at least rows / per + `more` of them (floor), since
-// floor((a + n) / per) - floor(a / per) >= floor(n / per).
-__device__ __forceinline__ int64_t item_start(int64_t cu, int b, int per, int more) {
-  return cu / per + (int64_t)b * more;
+// sequence b, of `mul` rows per token, owns items item_start(cu[b], b) ..
+// item_start(cu[b + 1], b + 1) - 1, at least rows / per + `more` of them (floor),
+// since floor((a + n) / per) - floor(a / per) >= floor(n / per).
+__device__ __forceinline__ int64_t item_start(int64_t cu, int b, int per, int more, int mul = 1) {
+  return cu * mul / per + (int64_t)b * more;
 }
 
 // The sequence that owns item x, or -1 (wave-uniform).
 __device__ __forceinline__ int find_item(const int32_t* cu, int n, int64_t total, int64_t x,
-                                         int per, int more) {
+                                         int per, int more, int mul = 1) {
   const int lane = threadIdx.x & 63;
   for (int base = 0; base < n; base += 64) {
     const int b = base + lane;
     const bool at_or_before =
-        b < n && item_start(clamp64(cu[b], 0, total), b, per, more) <= x;
+        b < n && item_start(clamp64(cu[b], 0, total), b, per, more, mul) <= x;
     const int cnt = __popcll(__ballot(at_or_before));
     if (cnt < 64)  // -1 before the first sequence's items
       return __builtin_amdgcn_readfirstlane(base + cnt - 1);

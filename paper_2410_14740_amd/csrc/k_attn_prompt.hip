@@ -14,21 +14,29 @@
 // {4h .. 4h + 3, 8 + 4h .. 8 + 4h + 3} of the 16, h = lane / 32, and V^T's A
 // operand is read in that order (transposing LDS reads, 4 tokens each).
 //
-// 128 query rows per workgroup, 32 per wave, two workgroups per CU (64 KB of
-// LDS and up to 256 registers each): the four waves share the key and value
-// tiles, loaded straight into LDS one tile ahead. The next tile's score
-// products are in the same stretch of code as this tile's softmax, which runs
-// beside them. Measured: 64 / 8 heads of 128, bf16, causal, 8192 + 2500 tokens
-// 1100 us, 1.09 PFLOP/s (a bf16 product of 8192^3 by the library: 1.25); 32
-// heads, fp16, seven prompts of 1 .. 2380 tokens 80 us; 40 heads, chunks of 512,
-// 300 and 77 rows against up to 3584 keys 75 us. What bounds it: the matrix
-// instructions are busy in 59% of the cycles, some vector or matrix instruction
-// in 80%; a workgroup alone on its CU takes 1.4 us per tile of keys, two
-// together 1.9 us for both, so the last two cases, whose longest rows are 38 and
-// 56 tiles, wait for those rows.
+// A row is one token's query head. The heads that share a key/value head lie in
+// the same tiles of rows, token by token, so that few tokens of many heads fill
+// them too and read their keys once (16 tokens of 64 / 8 heads on 65536 keys: 157
+// us with a head's rows to a tile, 86 so).
+// 128 rows per workgroup, 32 per wave, two workgroups per CU (64 KB of LDS and
+// up to 256 registers each): the four waves share the key and value tiles,
+// loaded straight into LDS one tile ahead. The next tile's score products are in
+// the same stretch of code as this tile's softmax, which runs beside them. Few
+// rows of many keys are cut along the keys (see Plan).
+//
+// Measured: 64 / 8 heads of 128, bf16, causal, 8192 + 2500 tokens 1110 us, 1.08
+// PFLOP/s (a bf16 product of 8192^3 by the library: 1.25); 32 heads, fp16, seven
+// prompts of 1 .. 2380 tokens 82 us; 40 heads, chunks of 512, 300 and 77 rows
+// against up to 3584 keys 76 us and a join of 4 that finds nothing to do. What
+// bounds it: the matrix instructions are busy in 59% of the cycles, some vector
+// or matrix instruction in 80%; a workgroup alone on its CU takes 1.4 us per tile
+// of keys, two together 1.9 us for both, so the last two cases, whose longest
+// rows are 38 and 56 tiles, wait for those rows.
+#include <algorithm>
 #include <type_traits>
 
 #include "attn_device.h"
+#include "wave_ops.h"
 
 namespace m2c {
 
@@ -39,19 +47,32 @@ struct PromptArgs {
   const int32_t *cu_q, *cu_k;
   int64_t total_q, total_k;
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // bytes
-  float c;     // scale * log2 e
-  int n_seqs, n_heads, group, causal;
+  float* part_o;    // [2 extra][units][kRows][D] unnormalized outputs of parts of rows
+  float2* part_ml;  // [2 extra][units][kRows] their m and l
+  float c;          // scale * log2 e
+  int n_seqs, n_heads, causal;
+  int pack;    // query heads of a key/value head whose rows lie in one tile: all, or 1
+  int units;   // n_heads / pack: what a row tile is taken for
+  int shared;  // of those, the ones with the same key/value head
+  int extra;   // parts beyond the first of a row tile that there is room for, per unit; 0: none are cut
 };
 
 namespace {
 
 constexpr int kTileK = 64;  // keys per tile
+constexpr int kWaves = 4, kRows = kWaves * 32;  // query rows per workgroup
 // Weights are taken as 2^(x - m + kLift), l and O alike, and m may stay up to
 // kSlack below the largest x. Rounded to fp16 the largest is then 2^14, and
 // weights down to 2^-24 of 2^m keep all their bits (2^-14 without the lift; a
 // long sequence of small weights beside one large one would lose them). It
 // cancels in O / l and is taken out of the log-sum-exp.
 constexpr float kSlack = 4.0f, kLift = 10.0f;
+
+constexpr int kShares = 512;    // workgroups that run at once: two per CU
+constexpr int kLeast = 8;       // tiles of a part at least, where rows are split
+constexpr int kJoins = 1024;    // workgroups of the join
+constexpr float kUneven = 3.0f;
+constexpr int kExtra = 1024;    // parts beyond the first of a row tile, all units
 
 // A raw buffer over `bytes` bytes at p: loads past its end give zeros.
 __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
@@ -102,19 +123,22 @@ __device__ __forceinline__ float wave_add(float v) {
 
 // The rows of one wave again, key by key, each row over the keys it sees only:
 // taken where a value that some of the rows must not see is an infinity or a
-// NaN, which a product with p = 0 would carry into them.
+// NaN, which a product with p = 0 would carry into them. part_o, part_ml (NULL
+// for whole rows): the wave's place of a part, which has the first `most` keys.
 template <bool BF, int D>
 __device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8_t* qb, const uint8_t* kb,
                                              const uint8_t* vb, uint8_t* ob, float* lse, int r0,
-                                             int ql, int kl) {
+                                             int rows, int off, int kl, int most, float* part_o,
+                                             float2* part_ml) {
   const int lane = threadIdx.x & 63;
   constexpr int E = D / 64;
-  for (int r = r0; r < r0 + 32 && r < ql; ++r) {
-    const int seen = min(kl, max(0, A.causal ? kl - ql + r + 1 : kl));
+  for (int r = r0; r < r0 + 32 && r < rows; ++r) {
+    const int tok = r / A.pack, hd = r - tok * A.pack;
+    const int seen = min(most, A.causal ? off + tok + 1 : kl);
     float q[E], o[E], m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      q[e] = unpack16<BF>(*(const uint16_t*)(qb + r * A.q_tok + (lane + 64 * e) * 2));
+      q[e] = unpack16<BF>(*(const uint16_t*)(qb + tok * A.q_tok + hd * A.q_head + (lane + 64 * e) * 2));
       o[e] = 0.0f;
     }
     for (int j = 0; j < seen; ++j) {
@@ -131,12 +155,22 @@ __device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8
         o[e] = o[e] * a + p * unpack16<BF>(*(const uint16_t*)(vb + j * A.v_tok + (lane + 64 * e) * 2));
       m = mn;
     }
+    if (part_o) {
+      const int col = r - r0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = lane + 64 * e;  // where the lane that has it in the products puts it
+        part_o[(d / 8 * 64 + (d / 4 & 1) * 32 + col) * 4 + d % 4] = ldexpf(o[e], (int)kLift);
+      }
+      if (lane == 0) part_ml[col] = make_float2(m, ldexpf(l, (int)kLift));
+      continue;
+    }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      *(uint16_t*)(ob + r * A.o_tok + (lane + 64 * e) * 2) = (uint16_t)pack16<BF>(o[e] * inv, 0.0f);
+      *(uint16_t*)(ob + tok * A.o_tok + hd * A.o_head + (lane + 64 * e) * 2) = (uint16_t)pack16<BF>(o[e] * inv, 0.0f);
     if (lse && lane == 0)
-      lse[(int64_t)r * A.n_heads] = (m + log2_fast(l)) * kLn2;
+      lse[(int64_t)tok * A.n_heads + hd] = (m + log2_fast(l)) * kLn2;
   }
 }
 
@@ -145,7 +179,6 @@ __device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8
 // keys, longest first, and in each a causal mask's longest rows first, so that
 // the last workgroups to start are short ones. More than 64 sequences (a lane
 // each) are taken as they come.
-template <int ROWS>
 __device__ __forceinline__ int find_tile(const PromptArgs& A, int x, int* qt) {
   const int lane = threadIdx.x & 63, n = A.n_seqs;
   int b, j, tiles;
@@ -154,7 +187,7 @@ __device__ __forceinline__ int find_tile(const PromptArgs& A, int x, int* qt) {
     if (lane < n) {
       const int64_t lo = clamp64(A.cu_q[lane], 0, A.total_q), hi = clamp64(A.cu_q[lane + 1], lo, A.total_q);
       const int64_t k0 = clamp64(A.cu_k[lane], 0, A.total_k), k1 = clamp64(A.cu_k[lane + 1], k0, A.total_k);
-      nt = (int)((hi - lo + ROWS - 1) / ROWS);
+      nt = ((int)(hi - lo) * A.pack + kRows - 1) / kRows;
       kl = (int)(k1 - k0);
     }
     int start = 0;  // tiles of the sequences before the lane's
@@ -168,20 +201,88 @@ __device__ __forceinline__ int find_tile(const PromptArgs& A, int x, int* qt) {
     j = x - __builtin_amdgcn_readlane(start, b);
     tiles = __builtin_amdgcn_readlane(nt, b);
   } else {
-    b = find_item(A.cu_q, n, A.total_q, x, ROWS, 1);
+    b = find_item(A.cu_q, n, A.total_q, x, kRows, 1, A.pack);
     if (b < 0) return -1;
     const int64_t lo = clamp64(A.cu_q[b], 0, A.total_q), hi = clamp64(A.cu_q[b + 1], lo, A.total_q);
-    tiles = (int)((hi - lo + ROWS - 1) / ROWS);
-    j = x - (int)item_start(lo, b, ROWS, 1);
+    tiles = ((int)(hi - lo) * A.pack + kRows - 1) / kRows;
+    j = x - (int)item_start(lo, b, kRows, 1, A.pack);
     if (j >= tiles) return -1;
   }
   *qt = A.causal ? tiles - 1 - j : j;
   return b;
 }
 
-template <bool BF, int D, int NW>
-__global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const PromptArgs A) {
-  constexpr int kRows = NW * 32;           // query rows per workgroup
+// Where a row tile sees kUneven times as many tiles of keys as each of the
+// workgroups that run at once has to take, row tiles are cut along their keys
+// into parts of such a share, joined by a second launch. Lane b of a wave holds
+// sequence b: the last `keyed` of its row tiles see some key, and each is cut
+// into at most `per` parts of up to `most` tiles; the sequence's items are start
+// .. in the order of find_tile, a row tile's parts one after another. (Measured,
+// in us without and with cuts: 1 head, 6000 rows, longest 21 shares 98, 33; 32 / 8
+// heads, 512 rows on 16384 keys, 4 shares 258, 144; 8 heads of 64, 4000 rows, 3.8
+// shares 51, 48; 40 heads, 2.2 shares 71, 94. Parts of a half share are as fast or
+// slower by up to a tenth.)
+struct Plan {
+  int rows, keyed, per, start;
+  int row_start, slot_start;  // its first among the row tiles and parts of the sequences that are cut
+  int most;
+};
+
+__device__ __forceinline__ Plan plan_of(const PromptArgs& A) {
+  const int lane = threadIdx.x & 63, n = A.n_seqs;
+  Plan P = {};
+  int kl = -1, kt = 0;
+  float work = 0.0f;
+  if (lane < n) {
+    const int64_t lo = clamp64(A.cu_q[lane], 0, A.total_q), hi = clamp64(A.cu_q[lane + 1], lo, A.total_q);
+    const int64_t k0 = clamp64(A.cu_k[lane], 0, A.total_k), k1 = clamp64(A.cu_k[lane + 1], k0, A.total_k);
+    const int rows = (int)(hi - lo) * A.pack;
+    kl = (int)(k1 - k0);
+    P.rows = (rows + kRows - 1) / kRows;
+    kt = (kl + kTileK - 1) / kTileK;
+    const int off = kl - (int)(hi - lo);
+    const int empty = kl == 0 ? P.rows : A.causal && off < 0 ? -off * A.pack / kRows : 0;
+    P.keyed = P.rows - empty;
+    int first = kt;  // tiles the first of them sees
+    if (A.causal) {
+      const int last = min(rows, (empty + 1) * kRows) - 1;
+      first = (min(kl, max(0, off + last / A.pack + 1)) + kTileK - 1) / kTileK;
+    }
+    work = 0.5f * (float)P.keyed * ((float)first + (float)kt);
+  }
+  work = add_xor32(add_xor16(work));
+  work += row_xor<1>(work), work += row_xor<2>(work), work += row_xor<4>(work), work += row_xor<8>(work);
+  const float share = work * (float)A.units * (1.0f / kShares);
+  const bool even = (float)wave_max((uint32_t)kt) <= kUneven * share;
+  P.most = even ? 1 << 25 : (int)fminf(fmaxf((float)kLeast, ceilf(share)), 0x1p25f);
+  P.most = __builtin_amdgcn_readfirstlane(P.most);
+  int cut;
+  for (;; P.most *= 2) {  // ends: no sequence has more than 2^24 tiles
+    P.per = P.keyed > 0 ? (kt + P.most - 1) / P.most : 1;
+    cut = P.per > 1 ? P.keyed * P.per : 0;
+    const uint32_t extra = P.per > 1 ? (uint32_t)(cut - P.keyed) : 0u;
+    if (__builtin_amdgcn_readlane(wave_incl_scan(extra), 63) <= A.extra) break;
+  }
+  const int items = P.per > 1 ? cut + P.rows - P.keyed : P.rows;
+  const int cut_rows = P.per > 1 ? P.keyed : 0;
+  for (int i = 0; i < n; ++i) {
+    const int k2 = __builtin_amdgcn_readlane(kl, i), n2 = __builtin_amdgcn_readlane(items, i);
+    const int r2 = __builtin_amdgcn_readlane(cut_rows, i), c2 = __builtin_amdgcn_readlane(cut, i);
+    if (k2 > kl || (k2 == kl && i < lane)) P.start += n2, P.row_start += r2, P.slot_start += c2;
+  }
+  return P;
+}
+
+// The kernel's arguments by a pointer that the compiler cannot tell from others.
+__device__ __forceinline__ const PromptArgs* args_again() {
+  uint64_t p = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return (const PromptArgs*)(const __attribute__((address_space(4))) PromptArgs*)(uintptr_t)p;
+}
+
+template <bool BF, int D, bool SPLIT>
+__global__ void __launch_bounds__(kWaves * 64, 2) prompt_attention_kernel(const PromptArgs A) {
+  constexpr int NW = kWaves;
   constexpr int kRowBytes = D * 2, kChunks = D / 8;
   constexpr int kTileBytes = kTileK * kRowBytes;
   constexpr int kLoads = kTileBytes / (NW * 1024);  // per wave, for K and for V
@@ -192,35 +293,67 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
   // Consecutive workgroups go round the eight XCDs: they take the heads of one
   // query tile, and where the key/value heads divide by eight, each XCD keeps
   // the same ones, so that its L2 holds their keys and values for all tiles.
-  const int G = A.group, n_kv = A.n_heads / G;
-  const int x = blockIdx.x / A.n_heads, r = blockIdx.x - x * A.n_heads;
-  const int per_xcd = n_kv / 8;
-  const int hr = n_kv % 8 == 0 ? (r & 7) * per_xcd * G + (r >> 3) : r;
-  const int kvh = hr / G, head = hr;
-  int qt;
-  const int b = find_tile<kRows>(A, x, &qt);
-  if (b < 0) return;
+  const int n_kv = A.units / A.shared;
+  const int x = blockIdx.x / A.units, r = blockIdx.x - x * A.units;
+  const int unit = n_kv % 8 == 0 ? (r & 7) * (A.units / 8) + (r >> 3) : r;
+  const int kvh = unit / A.shared, head = unit * A.pack;
+  int qt, b, part = 0, most = 0, slot = 0;
+  if constexpr (SPLIT) {
+    const Plan P = plan_of(A);
+    const int items = P.per > 1 ? P.keyed * P.per + P.rows - P.keyed : P.rows;
+    const unsigned long long own = __ballot(x >= P.start && x < P.start + items);
+    if (!own) return;
+    b = __builtin_amdgcn_readfirstlane(__ffsll(own) - 1);
+    const int j = x - __builtin_amdgcn_readlane(P.start, b), per = __builtin_amdgcn_readlane(P.per, b);
+    const int rows = __builtin_amdgcn_readlane(P.rows, b), keyed = __builtin_amdgcn_readlane(P.keyed, b);
+    int i = j;
+    if (per > 1 && j < keyed * per) {
+      i = j / per;
+      part = j - i * per;
+      most = P.most;
+      slot = __builtin_amdgcn_readlane(P.slot_start, b) + j;
+    } else if (per > 1) {
+      i = j - keyed * per + keyed;
+    }
+    qt = rows - 1 - i;
+  } else {
+    b = find_tile(A, x, &qt);
+    if (b < 0) return;
+  }
   const int64_t q_lo = clamp64(A.cu_q[b], 0, A.total_q), q_hi = clamp64(A.cu_q[b + 1], q_lo, A.total_q);
   const int64_t k_lo = clamp64(A.cu_k[b], 0, A.total_k), k_hi = clamp64(A.cu_k[b + 1], k_lo, A.total_k);
-  const int ql = (int)(q_hi - q_lo), kl = (int)(k_hi - k_lo);
+  const int ql = (int)(q_hi - q_lo);
+  int kl = (int)(k_hi - k_lo);
 
   const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint8_t* qb = A.q + q_lo * A.q_tok + head * A.q_head;
   const uint8_t* kb = A.k + k_lo * A.k_tok + kvh * A.k_head;
   const uint8_t* vb = A.v + k_lo * A.v_tok + kvh * A.v_head;
-  uint8_t* ob = A.out + q_lo * A.o_tok + head * A.o_head;
-  float* lse = A.lse ? A.lse + q_lo * A.n_heads + head : nullptr;
 
+  const int rows = ql * A.pack;
   const int r0 = qt * kRows + wave * 32;  // the wave's first row
   const int row = r0 + col;               // the lane's
+  const int tok = min(row, rows - 1) / A.pack, hd = min(row, rows - 1) - tok * A.pack;
   // keys the workgroup, the wave's first and last row, and the lane's row see
-  const int off = kl - ql;
-  const int wg_seen = A.causal ? min(kl, max(0, off + min(ql, (qt + 1) * kRows))) : kl;
-  const int wv_lo = A.causal ? min(kl, max(0, off + r0 + 1)) : kl;
-  const int wv_hi = r0 >= ql ? 0 : A.causal ? min(kl, max(0, off + min(ql, r0 + 32))) : kl;
-  const int seen = A.causal ? min(kl, max(0, off + row + 1)) : kl;
-  const int nt = (wg_seen + kTileK - 1) / kTileK;
+  int off = kl - ql;
+  auto seen_by = [&](int r) { return A.causal ? min(kl, max(0, off + r / A.pack + 1)) : kl; };
+  const int wg_seen = seen_by(min(rows, (qt + 1) * kRows) - 1);
+  const int tiles = (wg_seen + kTileK - 1) / kTileK;
+  int nt = tiles, parts = 1;
+  if constexpr (SPLIT) {
+    if (most) parts = max(1, (tiles + most - 1) / most);
+    if (part >= parts) return;
+    // from here on the keys count from the part's first
+    const int ta = (int)((int64_t)part * tiles / parts);
+    nt = (int)((int64_t)(part + 1) * tiles / parts) - ta;
+    kb += (int64_t)ta * kTileK * A.k_tok;
+    vb += (int64_t)ta * kTileK * A.v_tok;
+    kl -= ta * kTileK, off -= ta * kTileK;
+  }
+  const int wv_lo = seen_by(r0);
+  const int wv_hi = r0 >= rows ? 0 : seen_by(min(rows, r0 + 32) - 1);
+  int seen = 0;  // the lane's, set before the masked tiles
 
   // global -> LDS: load i of a wave takes rows (i NW + wave) kLoadRows .. of a
   // tile; the tile's buffer ends with the sequence, so rows past it are zeros
@@ -241,7 +374,7 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
 
   u32x4 qf[KS];
   {
-    const uint8_t* qr = qb + (int64_t)min(row, ql - 1) * A.q_tok + h * 16;
+    const uint8_t* qr = qb + tok * A.q_tok + hd * A.q_head + h * 16;
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = *(const u32x4*)(qr + s * 32);
     // wait for them here: a wait inside the loop would also wait for its tiles
@@ -353,7 +486,7 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
 
   // Tile t needs V(t) and K(t + 1). Waves pass the barriers of the loops
   // together, each with its own number of tiles in the first.
-  const int plain = r0 >= ql ? 0 : wv_lo / kTileK;  // tiles that every row of the wave sees whole
+  const int plain = r0 >= rows ? 0 : min(nt, wv_lo / kTileK);  // tiles that every row of the wave sees whole
   auto arrive = [&](int t) {
     // this wave's loads have landed, and its reads of K(t) and V(t - 1) are done
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -379,6 +512,13 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
     arrive(t + 1);
     compute(t + 1, s1, s0, std::false_type());
   }
+  // What only the masked tiles and the end need is computed again, not kept in
+  // registers through the loop above (the compiler, short of them, would order
+  // its score products before the softmax instead of beside it).
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int row2 = r0 + (tid & 31);
+  seen = seen_by(min(row2, rows - 1));
   for (; t < nt; ++t) {
     arrive(t);
     if (t * kTileK < wv_hi) {
@@ -387,17 +527,40 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
       for (int i = 0; i < 2; ++i) s0[i] = s1[i];
     }
   }
+  const PromptArgs& B = *args_again();
+  const int64_t first = clamp64(B.cu_q[b], 0, B.total_q);
+  uint8_t* ob = B.out + first * B.o_tok + head * B.o_head;
+  float* lse = B.lse ? B.lse + first * B.n_heads + head : nullptr;
   constexpr uint32_t kInf = BF ? 0x7f80u : 0x7c00u;
   const bool bad = __ballot((worst & 0xffffu) >= kInf || (worst >> 16) >= kInf) != 0;
-  if (r0 >= ql) return;
-  if (bad && A.causal) {
-    wave_rows_plain<BF, D>(A, qb, kb, vb, ob, lse, r0, ql, kl);
+  if (r0 >= rows) return;
+  float* part_o = nullptr;
+  float2* part_ml = nullptr;
+  if (SPLIT && parts > 1) {
+    const int64_t at = ((int64_t)slot * B.units + unit) * kWaves + wave;
+    part_o = B.part_o + at * (32 * D);
+    part_ml = B.part_ml + at * 32;
+  }
+  if (bad && B.causal) {
+    wave_rows_plain<BF, D>(B, B.q + first * B.q_tok + head * B.q_head, kb, vb, ob, lse, r0, rows, off, kl,
+                           min(kl, nt * kTileK), part_o, part_ml);
     return;
   }
-  if (row >= ql) return;
   l = add_xor32(l);
+  if (SPLIT && parts > 1) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(part_o + ((dt * 4 + i) * 64 + lane) * 4) =
+            f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+    if (h == 0) part_ml[col] = make_float2(m, l);
+    return;
+  }
+  if (row2 >= rows) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  uint8_t* orow = ob + (int64_t)row * A.o_tok + h * 8;
+  const int o_tok = row2 / B.pack, o_hd = row2 - o_tok * B.pack;
+  uint8_t* orow = ob + o_tok * B.o_tok + o_hd * B.o_head + h * 8;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -407,20 +570,121 @@ __global__ void __launch_bounds__(NW * 64, 2) prompt_attention_kernel(const Prom
       w[1] = pack16<BF>(o[dt][4 * i + 2] * inv, o[dt][4 * i + 3] * inv);
       *(u32x2*)(orow + dt * 64 + i * 16) = w;
     }
-  if (lse && h == 0) lse[(int64_t)row * A.n_heads] = (m - kLift + log2_fast(l)) * kLn2;
+  if (lse && h == 0) lse[(int64_t)o_tok * B.n_heads + o_hd] = (m - kLift + log2_fast(l)) * kLn2;
 }
 
-template <bool BF, int D, int NW>
-hipError_t launch_tile(PromptArgs& A, hipStream_t stream) {
-  const int64_t items = A.total_q / (NW * 32) + A.n_seqs;
-  const int64_t grid = items * A.n_heads;
+// Joins the parts of the row tiles that were cut: 32 dimensions of 128 rows per
+// workgroup, each lane with the elements it had as a lane of the parts.
+template <bool BF, int D>
+__global__ void __launch_bounds__(kWaves * 64) prompt_join_kernel(const PromptArgs A) {
+  constexpr int DT = D / 32;
+  const Plan P = plan_of(A);
+  for (int id = blockIdx.x;; id += gridDim.x) {  // ends past the row tiles that were cut
+    const int x = id / (A.units * DT), r = id - x * (A.units * DT);
+    const int unit = r / DT, dt = r - unit * DT;
+    const unsigned long long own = __ballot(P.per > 1 && x >= P.row_start && x < P.row_start + P.keyed);
+    if (!own) return;
+    const int b = __builtin_amdgcn_readfirstlane(__ffsll(own) - 1);
+    const int i = x - __builtin_amdgcn_readlane(P.row_start, b), per = __builtin_amdgcn_readlane(P.per, b);
+    const int qt = __builtin_amdgcn_readlane(P.rows, b) - 1 - i;
+    const int64_t q_lo = clamp64(A.cu_q[b], 0, A.total_q), q_hi = clamp64(A.cu_q[b + 1], q_lo, A.total_q);
+    const int64_t k_lo = clamp64(A.cu_k[b], 0, A.total_k), k_hi = clamp64(A.cu_k[b + 1], k_lo, A.total_k);
+    const int ql = (int)(q_hi - q_lo), kl = (int)(k_hi - k_lo);
+    const int rows = ql * A.pack, last = min(rows, (qt + 1) * kRows) - 1;
+    const int seen = A.causal ? min(kl, max(0, kl - ql + last / A.pack + 1)) : kl;
+    const int tiles = (seen + kTileK - 1) / kTileK, parts = (tiles + P.most - 1) / P.most;
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = qt * kRows + wave * 32 + col;
+    if (parts > 1 && row < rows) {
+      const int64_t slot = ((int64_t)__builtin_amdgcn_readlane(P.slot_start, b) + i * per) * A.units + unit;
+      const float2* ml = A.part_ml + (slot * kWaves + wave) * 32 + col;
+      const float* po = A.part_o + (slot * kWaves + wave) * (32 * D) + (dt * 256 + lane) * 4;
+      const int64_t step = (int64_t)A.units * kWaves * 32;  // rows from part to part
+      float M = -INFINITY, L = 0.0f;
+      for (int p = 0; p < parts; ++p) M = fmaxf(M, ml[p * step].x);
+      const float mu = M == -INFINITY ? 0.0f : M;
+      f32x4 y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+      for (int p = 0; p < parts; ++p) {
+        const float2 v = ml[p * step];
+        const float f = exp2_fast(v.x - mu);
+        L = fmaf(v.y, f, L);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f32x4 a = *(const f32x4*)(po + p * step * D + k * 256);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[k][e] = fmaf(a[e], f, y[k][e]);
+        }
+      }
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      const int64_t tok = q_lo + row / A.pack;
+      const int head = unit * A.pack + row % A.pack;
+      uint8_t* orow = A.out + tok * A.o_tok + head * A.o_head + dt * 64 + h * 8;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const u32x2 w = {pack16<BF>(y[k][0] * inv, y[k][1] * inv), pack16<BF>(y[k][2] * inv, y[k][3] * inv)};
+        *(u32x2*)(orow + k * 16) = w;
+      }
+      if (A.lse && h == 0 && dt == 0)
+        A.lse[tok * A.n_heads + head] = (M - kLift + log2_fast(L)) * kLn2;
+    }
+  }
+}
+
+int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+
+int pack_of(const m2c_attn_desc* D, int64_t total_q) {
+  const int group = D->n_heads / D->n_kv_heads;
+  return total_q * group <= 1 << 30 ? group : 1;  // rows of a sequence fit 32 bits
+}
+
+// Parts beyond the first of a row tile to make room for, per unit, or 0. (A row
+// tile that is cut has at least one, so there are at most twice as many parts.
+// With a share a part they are at most 1024: a sequence's row tiles see half of
+// its longest's tiles or more on average.)
+int extra_of(const m2c_attn_desc* D, bool self, int n_seqs, int64_t total_q, int64_t total_k) {
+  if (n_seqs > 64) return 0;
+  const int pack = pack_of(D, total_q), units = D->n_heads / pack;
+  const int64_t tiles = (total_k + kTileK - 1) / kTileK, rows = total_q * pack / kRows + n_seqs;
+  if (tiles <= kLeast) return 0;
+  // Of lq queries with as many keys or more a row tile sees half the longest's
+  // tiles or more on average: where they are so many, none is cut. As many keys
+  // as queries in all are taken to be the same sequences.
+  const int64_t lq = n_seqs == 1 && total_q <= total_k ? total_q
+                     : self || total_q == total_k      ? D->max_q
+                                                       : 0;
+  if ((float)(lq * D->n_heads) * kUneven >= (float)(kShares * 2 * kRows)) return 0;
+  const int64_t most = rows * ((tiles - 1) / kLeast);
+  return (int)std::min<int64_t>((kExtra + units - 1) / units, most);
+}
+
+template <bool BF, int D>
+hipError_t launch_rows(PromptArgs& A, hipStream_t stream) {
+  const int64_t grid = (A.total_q * A.pack / kRows + A.n_seqs + A.extra) * A.units;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((prompt_attention_kernel<BF, D, NW>), dim3((uint32_t)grid), dim3(NW * 64), 0,
+  if (!A.extra) {
+    hipLaunchKernelGGL((prompt_attention_kernel<BF, D, false>), dim3((uint32_t)grid), dim3(kWaves * 64), 0,
+                       stream, A);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((prompt_attention_kernel<BF, D, true>), dim3((uint32_t)grid), dim3(kWaves * 64), 0,
                      stream, A);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((prompt_join_kernel<BF, D>), dim3(kJoins), dim3(kWaves * 64), 0, stream, A);
   return hipGetLastError();
 }
 
 }  // namespace
+
+int64_t prompt_workspace(const m2c_attn_desc* D, bool self, int n_seqs, int64_t total_q, int64_t total_k) {
+  const int64_t parts = 2 * (int64_t)extra_of(D, self, n_seqs, total_q, total_k) *
+                        (D->n_heads / pack_of(D, total_q));
+  return round256(parts * kRows * 8) + parts * kRows * D->head_dim * 4;
+}
 
 hipError_t launch_prompt_attention(const m2c_attn_desc* D, const void* q, const void* k,
                                    const void* v, const int32_t* cu_q, const int32_t* cu_k,
@@ -443,11 +707,16 @@ hipError_t launch_prompt_attention(const m2c_attn_desc* D, const void* q, const 
   A.c = (D->scale > 0.0f ? D->scale : 1.0f / sqrtf((float)D->head_dim)) * kLog2e;
   A.n_seqs = n_seqs;
   A.n_heads = D->n_heads;
-  A.group = D->n_heads / D->n_kv_heads;
+  A.pack = pack_of(D, total_q);
+  A.units = D->n_heads / A.pack;
+  A.shared = A.units / D->n_kv_heads;
   A.causal = D->causal;
+  A.extra = D->workspace ? extra_of(D, cu_q == cu_k, n_seqs, total_q, total_k) : 0;
+  A.part_ml = (float2*)D->workspace;
+  A.part_o = (float*)((uint8_t*)D->workspace + round256(2 * (int64_t)A.extra * A.units * kRows * 8));
   if (D->dtype == M2C_DTYPE_BF16)
-    return D->head_dim == 128 ? launch_tile<true, 128, 4>(A, stream) : launch_tile<true, 64, 4>(A, stream);
-  return D->head_dim == 128 ? launch_tile<false, 128, 4>(A, stream) : launch_tile<false, 64, 4>(A, stream);
+    return D->head_dim == 128 ? launch_rows<true, 128>(A, stream) : launch_rows<true, 64>(A, stream);
+  return D->head_dim == 128 ? launch_rows<false, 128>(A, stream) : launch_rows<false, 64>(A, stream);
 }
 
 }  // namespace m2c

@@ -182,323 +182,323 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
     flat_end = S.first_of(blockIdx.x + 1);
   }
   do {  // the rows of a share
-  int b, rt, s_id, len, ua, ub, chunk, step, page0 = -1, unit0 = -1;
-  int64_t part;
-  bool whole;
-  if constexpr (EVEN) {
-    const int rows = C.n_kv_heads * A.tiles;
-    b = __ffsll((unsigned long long)__ballot(flat >= S.start && flat < S.start + S.cost * rows)) - 1;
-    const uint32_t cost = __builtin_amdgcn_readlane(S.cost, b);
-    const uint32_t at = flat - __builtin_amdgcn_readlane(S.start, b);
-    s_id = __builtin_amdgcn_readlane(S.s, b);
-    len = __builtin_amdgcn_readlane(S.len, b);
-    rt = (int)(at / cost);
-    ua = (int)(at - rt * cost);
-    const uint32_t take = min(cost - ua, flat_end - flat);
-    whole = take == cost;
-    ub = min(ua + (int)take, units_of(len, BT, UNIT));
-    chunk = step = 64 * kWaves;
-    part = (int64_t)b * rows + rt + blockIdx.x;  // a next row or a next share: one more
-    flat += take;
-  } else {
-    const int row = blockIdx.x / A.splits, split = blockIdx.x - row * A.splits;
-    const int rows = C.n_kv_heads * A.tiles;
-    b = row / rows, rt = row - b * rows;
-    s_id = A.seqs ? A.seqs[b] : b;
-    if (s_id < 0 || s_id >= C.n_seqs) s_id = -1;
-    // The first chunk's pages, asked for before the length is known: lane i of
-    // a wave has its i-th unit's.
-    unit0 = split * A.chunk + wave + kWaves * lane;
-    const int64_t at = ((int64_t)max(s_id, 0) * C.n_kv_heads + rt / A.tiles) * C.max_blocks;
-    page0 = (unit0 >> halves) < C.max_blocks ? C.table[at + (unit0 >> halves)] : -1;
-    len = s_id >= 0 ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * BT) : 0;
-    ua = split * A.chunk, ub = units_of(len, BT, UNIT);
-    chunk = A.chunk, step = A.splits * A.chunk;
-    part = blockIdx.x;
-    whole = A.splits == 1;
-    if (!whole && ua >= ub) return;  // a part without tokens; the join knows
-  }
-  if (s_id < 0 && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
-  const int s = max(s_id, 0);
-  const int kvh = rt / A.tiles, ht = rt - kvh * A.tiles, rk = b * C.n_kv_heads + kvh;
-  const int heads = min(16, A.group - ht * 16);           // query heads of this tile
-  const int h0 = kvh * A.group + ht * 16;                 // the first
-  const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
-  const int32_t* table = C.table + sh * C.max_blocks;
-  const int full = (len / BT) << halves;                  // units that lie in pages
-  float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
-                        : nullptr;
-
-  // queries: column = head, a step's elements where the key loads have them
-  u32x4 qf[KS];
-  const uint8_t* qrow = A.q + b * A.q_row + (h0 + min(col, heads - 1)) * A.q_head;
-#pragma unroll
-  for (int k = 0; k < KS; ++k) qf[k] = *(const u32x4*)(qrow + ((k / 2) * 64 + qr * 16 + (k & 1) * 8) * 2);
-  float qc = A.c;
-  if constexpr (BF) {
-    uint32_t big = 0;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t u = qf[k][w];
-        const uint32_t a = u & 0x7fffu, d = u >> 16 & 0x7fffu;
-        big = max(big, max(a < 0x7f80u ? a : 0u, d < 0x7f80u ? d : 0u));
-      }
-    big = max(big, (uint32_t)__shfl_xor((int)big, 16));
-    big = max(big, (uint32_t)__shfl_xor((int)big, 32));
-    const int ex = big >= 0x80u ? (int)(big >> 7) - 127 : big ? -126 : 14;  // the largest is below 2^(ex + 1)
-    const int up = 14 - ex;
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t u = qf[k][w];
-        qf[k][w] = pack16<false>(ldexpf(unpack16<true>(u & 0xffffu), up), ldexpf(unpack16<true>(u >> 16), up));
-      }
-    qc = ldexpf(A.c, -up);
-  }
-
-  f32x4 o[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m = -INFINITY, l = 0.0f;
-
-  for (int u0 = ua; u0 < ub; u0 += step) {
-    const int u1 = min(ub, u0 + chunk);
-    // A wave's units of the chunk are u0 + wave, + kWaves, .. (at most 64);
-    // lane i holds the page of its i-th, -1 for one that does not exist: page 0
-    // stands in with scales of 0, a block of zeros.
-    const int mine = u0 + wave + kWaves * lane;
-    int page = 0;
-    if (mine < min(u1, full)) {
-      page = mine == unit0 ? page0 : table[mine >> halves];
-      if (page < 0 || page >= C.n_pages) {
-        atomicOr(C.status, kKvBadIndex);
-        page = -1;
-      }
+    int b, rt, s_id, len, ua, ub, chunk, step, page0 = -1, unit0 = -1;
+    int64_t part;
+    bool whole;
+    if constexpr (EVEN) {
+      const int rows = C.n_kv_heads * A.tiles;
+      b = __ffsll((unsigned long long)__ballot(flat >= S.start && flat < S.start + S.cost * rows)) - 1;
+      const uint32_t cost = __builtin_amdgcn_readlane(S.cost, b);
+      const uint32_t at = flat - __builtin_amdgcn_readlane(S.start, b);
+      s_id = __builtin_amdgcn_readlane(S.s, b);
+      len = __builtin_amdgcn_readlane(S.len, b);
+      rt = (int)(at / cost);
+      ua = (int)(at - rt * cost);
+      const uint32_t take = min(cost - ua, flat_end - flat);
+      whole = take == cost;
+      ub = min(ua + (int)take, units_of(len, BT, UNIT));
+      chunk = step = 64 * kWaves;
+      part = (int64_t)b * rows + rt + blockIdx.x;  // a next row or a next share: one more
+      flat += take;
+    } else {
+      const int row = blockIdx.x / A.splits, split = blockIdx.x - row * A.splits;
+      const int rows = C.n_kv_heads * A.tiles;
+      b = row / rows, rt = row - b * rows;
+      s_id = A.seqs ? A.seqs[b] : b;
+      if (s_id < 0 || s_id >= C.n_seqs) s_id = -1;
+      // The first chunk's pages, asked for before the length is known: lane i of
+      // a wave has its i-th unit's.
+      unit0 = split * A.chunk + wave + kWaves * lane;
+      const int64_t at = ((int64_t)max(s_id, 0) * C.n_kv_heads + rt / A.tiles) * C.max_blocks;
+      page0 = (unit0 >> halves) < C.max_blocks ? C.table[at + (unit0 >> halves)] : -1;
+      len = s_id >= 0 ? (int)clamp64(C.len[s_id], 0, (int64_t)C.max_blocks * BT) : 0;
+      ua = split * A.chunk, ub = units_of(len, BT, UNIT);
+      chunk = A.chunk, step = A.splits * A.chunk;
+      part = blockIdx.x;
+      whole = A.splits == 1;
+      if (!whole && ua >= ub) return;  // a part without tokens; the join knows
     }
-    // Each register set is loaded for the next unit as soon as the products have
-    // taken it, so a wave keeps up to a unit's bytes in flight while it computes.
-    u32x4 kw[T][KL];
-    uint32_t vw[V2][8][VW];
-    auto unit_at = [&](int u, int pg) {
-      return ((int64_t)max(pg, 0) * BT + (u & halves) * UNIT) * D;
-    };
-    auto load_k = [&](int64_t at) {
-      const int8_t* kp = C.k_codes + at + col * D + qr * 16;
+    if (s_id < 0 && threadIdx.x == 0) atomicOr(C.status, kKvBadIndex);
+    const int s = max(s_id, 0);
+    const int kvh = rt / A.tiles, ht = rt - kvh * A.tiles, rk = b * C.n_kv_heads + kvh;
+    const int heads = min(16, A.group - ht * 16);           // query heads of this tile
+    const int h0 = kvh * A.group + ht * 16;                 // the first
+    const int64_t sh = (int64_t)s * C.n_kv_heads + kvh;
+    const int32_t* table = C.table + sh * C.max_blocks;
+    const int full = (len / BT) << halves;                  // units that lie in pages
+    float2* wsum = A.wsum ? A.wsum + (((int64_t)rk * C.max_blocks) << halves) * A.group + ht * 16 + col
+                          : nullptr;
+
+    // queries: column = head, a step's elements where the key loads have them
+    u32x4 qf[KS];
+    const uint8_t* qrow = A.q + b * A.q_row + (h0 + min(col, heads - 1)) * A.q_head;
 #pragma unroll
-      for (int t = 0; t < T; ++t)
+    for (int k = 0; k < KS; ++k) qf[k] = *(const u32x4*)(qrow + ((k / 2) * 64 + qr * 16 + (k & 1) * 8) * 2);
+    float qc = A.c;
+    if constexpr (BF) {
+      uint32_t big = 0;
 #pragma unroll
-        for (int k = 0; k < KL; ++k) kw[t][k] = *(const u32x4*)(kp + t * 16 * D + k * 64);
-    };
-    auto load_v = [&](int64_t at) {
-      const int8_t* vp = C.v_codes + at + qr * 4 * D + col * E;
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int v = 0; v < V2; ++v)
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t u = qf[k][w];
+          const uint32_t a = u & 0x7fffu, d = u >> 16 & 0x7fffu;
+          big = max(big, max(a < 0x7f80u ? a : 0u, d < 0x7f80u ? d : 0u));
+        }
+      big = max(big, (uint32_t)__shfl_xor((int)big, 16));
+      big = max(big, (uint32_t)__shfl_xor((int)big, 32));
+      const int ex = big >= 0x80u ? (int)(big >> 7) - 127 : big ? -126 : 14;  // the largest is below 2^(ex + 1)
+      const int up = 14 - ex;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int8_t* p = vp + (v * 32 + (j / 4) * 16 + j % 4) * D;
-          if constexpr (VW == 2) {
-            const u32x2 w = *(const u32x2*)p;
-            vw[v][j][0] = w[0], vw[v][j][1] = w[1];
-          } else {
-            vw[v][j][0] = *(const uint32_t*)p;
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t u = qf[k][w];
+          qf[k][w] = pack16<false>(ldexpf(unpack16<true>(u & 0xffffu), up), ldexpf(unpack16<true>(u >> 16), up));
+        }
+      qc = ldexpf(A.c, -up);
+    }
+
+    f32x4 o[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -INFINITY, l = 0.0f;
+
+    for (int u0 = ua; u0 < ub; u0 += step) {
+      const int u1 = min(ub, u0 + chunk);
+      // A wave's units of the chunk are u0 + wave, + kWaves, .. (at most 64);
+      // lane i holds the page of its i-th, -1 for one that does not exist: page 0
+      // stands in with scales of 0, a block of zeros.
+      const int mine = u0 + wave + kWaves * lane;
+      int page = 0;
+      if (mine < min(u1, full)) {
+        page = mine == unit0 ? page0 : table[mine >> halves];
+        if (page < 0 || page >= C.n_pages) {
+          atomicOr(C.status, kKvBadIndex);
+          page = -1;
+        }
+      }
+      // Each register set is loaded for the next unit as soon as the products have
+      // taken it, so a wave keeps up to a unit's bytes in flight while it computes.
+      u32x4 kw[T][KL];
+      uint32_t vw[V2][8][VW];
+      auto unit_at = [&](int u, int pg) {
+        return ((int64_t)max(pg, 0) * BT + (u & halves) * UNIT) * D;
+      };
+      auto load_k = [&](int64_t at) {
+        const int8_t* kp = C.k_codes + at + col * D + qr * 16;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+          for (int k = 0; k < KL; ++k) kw[t][k] = *(const u32x4*)(kp + t * 16 * D + k * 64);
+      };
+      auto load_v = [&](int64_t at) {
+        const int8_t* vp = C.v_codes + at + qr * 4 * D + col * E;
+#pragma unroll
+        for (int v = 0; v < V2; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int8_t* p = vp + (v * 32 + (j / 4) * 16 + j % 4) * D;
+            if constexpr (VW == 2) {
+              const u32x2 w = *(const u32x2*)p;
+              vw[v][j][0] = w[0], vw[v][j][1] = w[1];
+            } else {
+              vw[v][j][0] = *(const uint32_t*)p;
+            }
+          }
+      };
+      // Scales come by scalar loads: a wait for them does not wait for the pages.
+      typedef const __attribute__((address_space(4))) float* Scales;
+      const Scales k_scale = (Scales)(uintptr_t)C.k_scale, v_scale = (Scales)(uintptr_t)C.v_scale;
+      // One unit, page pg; MORE: then loads the one at `next`. (The last unit is a
+      // copy of the code, not a condition in it: where a load may be left out the
+      // compiler has to wait for all that may be in flight.)
+      auto process = [&](int u, int pg, int64_t next, auto more_t) {
+        constexpr bool MORE = decltype(more_t)::value;
+        const float ks = pg < 0 ? 0.0f : k_scale[pg], vs = pg < 0 ? 0.0f : v_scale[pg];
+        f32x4 x[T];
+        const float f = ks * qc;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            half2v a, d, e, g;
+            i8x4_to_h2(kw[t][k / 2][(k & 1) * 2], a, d);
+            i8x4_to_h2(kw[t][k / 2][(k & 1) * 2 + 1], e, g);
+            const u32x4 kf = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, d),
+                              __builtin_bit_cast(uint32_t, e), __builtin_bit_cast(uint32_t, g)};
+            x[t] = mfma16<false>(kf, qf[k], x[t]);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[t][r] *= f;
+        }
+        if constexpr (MORE) load_k(next);
+        asm volatile("" ::: "memory");
+        float sum;
+        const float alpha = softmax_step<T>(x, m, l, &sum);
+        if (wsum) {
+          sum = add_xor16(add_xor32(sum));
+          if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
+        }
+        u32x4 pf[V2];
+#pragma unroll
+        for (int v = 0; v < V2; ++v) pf[v] = pack_p<false>(x[2 * v], x[2 * v + 1]);
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          f32x4 acc[4];
+#pragma unroll
+          for (int v = 0; v < V2; ++v) {
+            uint32_t c[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] = vw[v][j][w] ^ 0x80808080u;
+            auto frag = [&](auto idx) {
+              constexpr int I = decltype(idx)::value;
+              const u32x4 vf = {pair_of<I>(c[0], c[1]), pair_of<I>(c[2], c[3]), pair_of<I>(c[4], c[5]),
+                                pair_of<I>(c[6], c[7])};
+              acc[I] = mfma16<false>(vf, pf[v], v == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[I]);
+            };
+            frag(std::integral_constant<int, 0>());
+            frag(std::integral_constant<int, 1>());
+            frag(std::integral_constant<int, 2>());
+            frag(std::integral_constant<int, 3>());
+          }
+#pragma unroll
+          for (int i2 = 0; i2 < 4; ++i2)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              o[w * 4 + i2][r] = fmaf(acc[i2][r], vs, o[w * 4 + i2][r] * alpha);
+        }
+        if constexpr (MORE) load_v(next);
+      };
+      const int end = min(u1, full);
+      if (u0 + wave < end) {
+        int pg = __builtin_amdgcn_readlane(page, 0);
+        const int64_t at = unit_at(u0 + wave, pg);
+        load_k(at);
+        asm volatile("" ::: "memory");  // in this order, so that a wait for the keys is for them alone
+        load_v(at);
+        int u = u0 + wave;
+        for (int i = 1; u + kWaves < end; u += kWaves, ++i) {
+          const int next = __builtin_amdgcn_readlane(page, i);
+          process(u, pg, unit_at(u + kWaves, next), std::true_type());
+          pg = next;
+        }
+        process(u, pg, 0, std::false_type());
+      }
+      // Units of the open block, from the 16-bit tail, 32 tokens at a time; rows
+      // past the length are zeros, whatever the tail holds there.
+      for (int u = max(u0 + wave, full + ((u0 + wave - full) & (kWaves - 1))); u < u1; u += kWaves) {
+        const int t_first = (u - full) * UNIT, rest = min(UNIT, len % BT - t_first);
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int part = 0; part < rest; part += 32) {
+          const int left = rest - part;
+          const uint8_t* kt = C.tail_k + (sh * BT + t_first + part) * (D * 2);
+          const uint8_t* vt = C.tail_v + (sh * BT + t_first + part) * (D * 2);
+          // every load is issued before the first is used, from the last token
+          // where there is none
+          typedef uint32_t Row __attribute__((ext_vector_type(E / 2)));
+          u32x4 qw[KS], kl[2][KS];
+          Row vl[8];
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const int el = (k / 2) * 64 + qr * 16 + (k & 1) * 8;
+            qw[k] = *(const u32x4*)(qrow + el * 2);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              kl[t][k] = *(const u32x4*)(kt + (min(t * 16 + col, left - 1) * D + el) * 2);
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            vl[j] = *(const Row*)(vt + (min((j / 4) * 16 + qr * 4 + j % 4, left - 1) * D + col * E) * 2);
+          __builtin_amdgcn_sched_barrier(0);
+          f32x4 x[2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const bool in = t * 16 + col < left;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+              x[t] = mfma16<BF>(in ? kl[t][k] : u32x4{0, 0, 0, 0}, qw[k], x[t]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              x[t][r] = t * 16 + qr * 4 + r < left ? x[t][r] * A.c : -INFINITY;
+          }
+          float part_sum;
+          const float alpha = softmax_step<2>(x, m, l, &part_sum);
+          sum = sum * alpha + part_sum;
+#pragma unroll
+          for (int i = 0; i < E; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
+          const u32x4 pf = pack_p<BF>(x[0], x[1]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if ((j / 4) * 16 + qr * 4 + j % 4 >= left) vl[j] = Row{};
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
+            const u32x4 vf = {__builtin_amdgcn_perm(vl[1][i / 2], vl[0][i / 2], sel),
+                              __builtin_amdgcn_perm(vl[3][i / 2], vl[2][i / 2], sel),
+                              __builtin_amdgcn_perm(vl[5][i / 2], vl[4][i / 2], sel),
+                              __builtin_amdgcn_perm(vl[7][i / 2], vl[6][i / 2], sel)};
+            o[i] = mfma16<BF>(vf, pf, o[i]);
           }
         }
-    };
-    // Scales come by scalar loads: a wait for them does not wait for the pages.
-    typedef const __attribute__((address_space(4))) float* Scales;
-    const Scales k_scale = (Scales)(uintptr_t)C.k_scale, v_scale = (Scales)(uintptr_t)C.v_scale;
-    // One unit, page pg; MORE: then loads the one at `next`. (The last unit is a
-    // copy of the code, not a condition in it: where a load may be left out the
-    // compiler has to wait for all that may be in flight.)
-    auto process = [&](int u, int pg, int64_t next, auto more_t) {
-      constexpr bool MORE = decltype(more_t)::value;
-      const float ks = pg < 0 ? 0.0f : k_scale[pg], vs = pg < 0 ? 0.0f : v_scale[pg];
-      f32x4 x[T];
-      const float f = ks * qc;
-#pragma unroll
-      for (int t = 0; t < T; ++t) {
-        x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          half2v a, d, e, g;
-          i8x4_to_h2(kw[t][k / 2][(k & 1) * 2], a, d);
-          i8x4_to_h2(kw[t][k / 2][(k & 1) * 2 + 1], e, g);
-          const u32x4 kf = {__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, d),
-                            __builtin_bit_cast(uint32_t, e), __builtin_bit_cast(uint32_t, g)};
-          x[t] = mfma16<false>(kf, qf[k], x[t]);
+        if (wsum) {
+          sum = add_xor16(add_xor32(sum));
+          if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[t][r] *= f;
-      }
-      if constexpr (MORE) load_k(next);
-      asm volatile("" ::: "memory");
-      float sum;
-      const float alpha = softmax_step<T>(x, m, l, &sum);
-      if (wsum) {
-        sum = add_xor16(add_xor32(sum));
-        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
-      }
-      u32x4 pf[V2];
-#pragma unroll
-      for (int v = 0; v < V2; ++v) pf[v] = pack_p<false>(x[2 * v], x[2 * v + 1]);
-#pragma unroll
-      for (int w = 0; w < VW; ++w) {
-        f32x4 acc[4];
-#pragma unroll
-        for (int v = 0; v < V2; ++v) {
-          uint32_t c[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) c[j] = vw[v][j][w] ^ 0x80808080u;
-          auto frag = [&](auto idx) {
-            constexpr int I = decltype(idx)::value;
-            const u32x4 vf = {pair_of<I>(c[0], c[1]), pair_of<I>(c[2], c[3]), pair_of<I>(c[4], c[5]),
-                              pair_of<I>(c[6], c[7])};
-            acc[I] = mfma16<false>(vf, pf[v], v == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[I]);
-          };
-          frag(std::integral_constant<int, 0>());
-          frag(std::integral_constant<int, 1>());
-          frag(std::integral_constant<int, 2>());
-          frag(std::integral_constant<int, 3>());
-        }
-#pragma unroll
-        for (int i2 = 0; i2 < 4; ++i2)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            o[w * 4 + i2][r] = fmaf(acc[i2][r], vs, o[w * 4 + i2][r] * alpha);
-      }
-      if constexpr (MORE) load_v(next);
-    };
-    const int end = min(u1, full);
-    if (u0 + wave < end) {
-      int pg = __builtin_amdgcn_readlane(page, 0);
-      const int64_t at = unit_at(u0 + wave, pg);
-      load_k(at);
-      asm volatile("" ::: "memory");  // in this order, so that a wait for the keys is for them alone
-      load_v(at);
-      int u = u0 + wave;
-      for (int i = 1; u + kWaves < end; u += kWaves, ++i) {
-        const int next = __builtin_amdgcn_readlane(page, i);
-        process(u, pg, unit_at(u + kWaves, next), std::true_type());
-        pg = next;
-      }
-      process(u, pg, 0, std::false_type());
-    }
-    // Units of the open block, from the 16-bit tail, 32 tokens at a time; rows
-    // past the length are zeros, whatever the tail holds there.
-    for (int u = max(u0 + wave, full + ((u0 + wave - full) & (kWaves - 1))); u < u1; u += kWaves) {
-      const int t_first = (u - full) * UNIT, rest = min(UNIT, len % BT - t_first);
-      float sum = 0.0f;
-#pragma unroll 1
-      for (int part = 0; part < rest; part += 32) {
-        const int left = rest - part;
-        const uint8_t* kt = C.tail_k + (sh * BT + t_first + part) * (D * 2);
-        const uint8_t* vt = C.tail_v + (sh * BT + t_first + part) * (D * 2);
-        // every load is issued before the first is used, from the last token
-        // where there is none
-        typedef uint32_t Row __attribute__((ext_vector_type(E / 2)));
-        u32x4 qw[KS], kl[2][KS];
-        Row vl[8];
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const int el = (k / 2) * 64 + qr * 16 + (k & 1) * 8;
-          qw[k] = *(const u32x4*)(qrow + el * 2);
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-            kl[t][k] = *(const u32x4*)(kt + (min(t * 16 + col, left - 1) * D + el) * 2);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          vl[j] = *(const Row*)(vt + (min((j / 4) * 16 + qr * 4 + j % 4, left - 1) * D + col * E) * 2);
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 x[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-          const bool in = t * 16 + col < left;
-#pragma unroll
-          for (int k = 0; k < KS; ++k)
-            x[t] = mfma16<BF>(in ? kl[t][k] : u32x4{0, 0, 0, 0}, qw[k], x[t]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            x[t][r] = t * 16 + qr * 4 + r < left ? x[t][r] * A.c : -INFINITY;
-        }
-        float part_sum;
-        const float alpha = softmax_step<2>(x, m, l, &part_sum);
-        sum = sum * alpha + part_sum;
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[i][r] *= alpha;
-        const u32x4 pf = pack_p<BF>(x[0], x[1]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if ((j / 4) * 16 + qr * 4 + j % 4 >= left) vl[j] = Row{};
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
-          const u32x4 vf = {__builtin_amdgcn_perm(vl[1][i / 2], vl[0][i / 2], sel),
-                            __builtin_amdgcn_perm(vl[3][i / 2], vl[2][i / 2], sel),
-                            __builtin_amdgcn_perm(vl[5][i / 2], vl[4][i / 2], sel),
-                            __builtin_amdgcn_perm(vl[7][i / 2], vl[6][i / 2], sel)};
-          o[i] = mfma16<BF>(vf, pf, o[i]);
-        }
-      }
-      if (wsum) {
-        sum = add_xor16(add_xor32(sum));
-        if (lane < heads) wsum[(int64_t)u * A.group] = make_float2(m, sum);
       }
     }
-  }
 
-  // Join the waves. Lane (col, qr) holds dimensions (4 qr + r) E + i of head col.
-  l = add_xor16(add_xor32(l));
-  if (lane < 16) mls[wave][col] = make_float2(m, l);
+    // Join the waves. Lane (col, qr) holds dimensions (4 qr + r) E + i of head col.
+    l = add_xor16(add_xor32(l));
+    if (lane < 16) mls[wave][col] = make_float2(m, l);
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int i = 0; i < E; i += 4)
-      *(f32x4*)&mrg[wave][col][(qr * 4 + r) * E + i] = f32x4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]};
-  __syncthreads();
-  const int hd = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * E;
-  if (hd < heads) {
-    float M = -INFINITY, L = 0.0f, fac[kWaves];
+      for (int i = 0; i < E; i += 4)
+        *(f32x4*)&mrg[wave][col][(qr * 4 + r) * E + i] = f32x4{o[i][r], o[i + 1][r], o[i + 2][r], o[i + 3][r]};
+    __syncthreads();
+    const int hd = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * E;
+    if (hd < heads) {
+      float M = -INFINITY, L = 0.0f, fac[kWaves];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mls[w][hd].x);
-    const float mu = M == -INFINITY ? 0.0f : M;
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, mls[w][hd].x);
+      const float mu = M == -INFINITY ? 0.0f : M;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      fac[w] = exp2_fast(mls[w][hd].x - mu);
-      L += mls[w][hd].y * fac[w];
-    }
-    float y[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-      for (int i = 0; i < E; ++i) y[i] = fmaf(mrg[w][hd][d0 + i], fac[w], y[i]);
-    if (whole) {
-      const int64_t at = (int64_t)b * A.n_heads + h0 + hd;
-      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-      uint32_t* po = (uint32_t*)(A.out + b * A.o_row + (h0 + hd) * A.o_head + d0 * 2);
-#pragma unroll
-      for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
-      if ((threadIdx.x & 15) == 0) {
-        if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
-        if (A.fin) A.fin[at] = make_float2(M, inv);
+      for (int w = 0; w < kWaves; ++w) {
+        fac[w] = exp2_fast(mls[w][hd].x - mu);
+        L += mls[w][hd].y * fac[w];
       }
-    } else {
-      const int64_t at = part * min(A.group, 16) + hd;
-      if ((threadIdx.x & 15) == 0) A.part_ml[at] = make_float2(M, L);
-      float* po = A.part_o + at * D + d0;
+      float y[E];
 #pragma unroll
-      for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+      for (int i = 0; i < E; ++i) y[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < E; ++i) y[i] = fmaf(mrg[w][hd][d0 + i], fac[w], y[i]);
+      if (whole) {
+        const int64_t at = (int64_t)b * A.n_heads + h0 + hd;
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        uint32_t* po = (uint32_t*)(A.out + b * A.o_row + (h0 + hd) * A.o_head + d0 * 2);
+#pragma unroll
+        for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
+        if ((threadIdx.x & 15) == 0) {
+          if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
+          if (A.fin) A.fin[at] = make_float2(M, inv);
+        }
+      } else {
+        const int64_t at = part * min(A.group, 16) + hd;
+        if ((threadIdx.x & 15) == 0) A.part_ml[at] = make_float2(M, L);
+        float* po = A.part_o + at * D + d0;
+#pragma unroll
+        for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
+      }
     }
-  }
-  if (EVEN) __syncthreads();  // the next row writes the same LDS
+    if (EVEN) __syncthreads();  // the next row writes the same LDS
   } while (EVEN && flat < flat_end);
 }
 

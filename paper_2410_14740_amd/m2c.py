@@ -92,7 +92,8 @@ class AttnDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "dtype", "n_heads", "n_kv_heads", "head_dim", "causal", "device")] + [
         ("scale", ctypes.c_float), ("max_q", ctypes.c_int32)] + [
-        (n, _I64x2) for n in ("q_stride", "k_stride", "v_stride", "out_stride")]
+        (n, _I64x2) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] + [
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 class KvCacheDesc(ctypes.Structure):
@@ -162,6 +163,7 @@ def load(path: str = LIB_PATH):
                                    ctypes.POINTER(I32), ctypes.POINTER(I32), P]),
         "m2c_prompt_attention": (I32, [ctypes.POINTER(AttnDesc), P, P, P, P, P, I32, I64, I64, P, P,
                                        P]),
+        "m2c_prompt_attention_workspace": (I64, [ctypes.POINTER(AttnDesc), P, P, I32, I64, I64]),
         "m2c_kv_reset": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P]),
         "m2c_kv_append": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, P, P, P, _I64x2, _I64x2,
                                 P]),
@@ -424,6 +426,13 @@ def m2c_prompt_attention(desc: AttnDesc, q, k, v, cu_q, cu_k, n_seqs: int, total
     _check(load().m2c_prompt_attention(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k),
                                        n_seqs, total_q, total_k, _ptr(out), _ptr(lse),
                                        _stream(stream)))
+
+
+def m2c_prompt_attention_workspace(desc: AttnDesc, cu_q, cu_k, n_seqs: int, total_q: int, total_k: int) -> int:
+    need = load().m2c_prompt_attention_workspace(desc, _ptr(cu_q), _ptr(cu_k), n_seqs, total_q, total_k)
+    if need < 0:
+        raise M2CError(M2C_ERR_INVALID_ARG, load().m2c_last_error().decode())
+    return need
 
 
 def m2c_kv_reset(cache: KvCacheDesc, seqs, n: int, stream=None):

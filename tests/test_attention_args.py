@@ -130,3 +130,21 @@ def test_workspace_sizes(lib):
     assert long >= 8 * 128 * 4 * 2 and ws(1, 0, 0) == long  # the capacity where no length is known
     assert ws(2, 0, 16384 * 64) >= long
     assert ws(1, 1, 64) >= 8 * 16384 * 8
+
+
+def test_prompt_workspace(lib):
+    """Room for parts of rows where some may see many more keys than others."""
+    need = lambda d, same, n, tq, tk: m2c.m2c_prompt_attention_workspace(d, P, P if same else 2 * P, n, tq, tk)  # noqa: E731
+    assert need(desc(), True, 1, 500, 500) == 0      # no row is long
+    assert need(desc(), False, 65, 9000, 90000) == 0  # more sequences than lanes
+    assert need(desc(n_heads=64, n_kv_heads=8, max_q=8192), True, 2, 10000, 10000) == 0  # enough rows
+    assert need(desc(), False, 1, 1, 100000) >= 2 * 8 * 128 * (128 + 2) * 4
+    assert need(desc(), True, 1, 0, 9000) == 0
+    with pytest.raises(m2c.M2CError) as e:
+        need(desc(max_q=-1), False, 1, 1, 100000)
+    assert e.value.status == m2c.M2C_ERR_INVALID_ARG and "max_q" in str(e.value)
+    for kw, status, needle in [(dict(workspace=P + 64, workspace_bytes=1 << 40), m2c.M2C_ERR_INVALID_ARG, "aligned"),
+                               (dict(workspace=P, workspace_bytes=4096), m2c.M2C_ERR_CAPACITY, "workspace")]:
+        with pytest.raises(m2c.M2CError) as e:
+            prompt(d=desc(**kw), cu_k=2 * P, tq=1, tk=100000)
+        assert e.value.status == status and needle in str(e.value)

@@ -115,6 +115,79 @@ def test_prompt(hq, hk, d, dt, ql, kl, causal):
     assert torch.equal(out, same)  # the same bits on every run
 
 
+SPLITS = [
+    # few rows and many keys: rows are cut along their keys
+    (2, 1, 128, BF16, [1], [5000], True),
+    (1, 1, 64, F16, [2], [769], True),                          # one part and a tile's first key
+    (4, 2, 64, F16, [130, 17, 1], [4000, 900, 3000], True),
+    (3, 3, 128, F16, [300, 0, 40], [4097, 2000, 1], False),
+    (1, 1, 128, F16, [3000], [2000], True),                     # row tiles without keys before those that are cut
+    (2, 2, 64, BF16, [1500, 700, 3000], [800, 2500, 3100], True),
+    (8, 1, 128, F16, [129], [6000], True),                      # a tile of one row
+    (64, 8, 64, BF16, [20, 5], [1500, 20000], True),
+]
+
+
+@pytest.mark.parametrize("hq,hk,d,dt,ql,kl,causal", SPLITS)
+def test_prompt_cut_along_the_keys(hq, hk, d, dt, ql, kl, causal):
+    say(f"prompt cut {hq}/{hk}x{d} {dt} {ql} {kl} causal={causal}")
+    q, k, v = rand((sum(ql), hq, d), dt, 4, 1.5), rand((sum(kl), hk, d), dt, 5), rand((sum(kl), hk, d), dt, 6)
+    cu, ck = starts(ql), starts(kl)
+    args = dict(causal=causal, return_lse=True, max_q=max(ql))
+    out, lse = prompt_attention(q, k, v, cu, ck, **args)
+    check_prompt(q, k, v, ql, kl, causal, out, lse)
+    assert all(map(torch.equal, (out, lse), prompt_attention(q, k, v, cu, ck, **args)))
+    # the same call without room for parts
+    desc = m2c.AttnDesc(m2c.DTYPE_BF16 if dt == BF16 else m2c.DTYPE_FP16, hq, hk, d, causal, 0, 0.0, 0)
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        setattr(desc, name + "_stride", t.stride()[:2])
+    whole, wlse = torch.empty_like(out), torch.empty_like(lse)
+    assert m2c.m2c_prompt_attention_workspace(desc, cu, ck, len(ql), sum(ql), sum(kl)) > 0
+    m2c.m2c_prompt_attention(desc, q, k, v, cu, ck, len(ql), sum(ql), sum(kl), whole, wlse)
+    check_prompt(q, k, v, ql, kl, causal, whole, wlse)
+
+
+@pytest.mark.parametrize("dt", [F16, BF16])
+@pytest.mark.parametrize("what", [math.inf, math.nan])
+def test_prompt_cut_masked_values_do_not_enter(dt, what):
+    """The keys that only some rows see lie in one part or in two."""
+    say(f"prompt cut masked {dt} {what}")
+    hq, hk, d, nq, nk = 2, 1, 64, 200, 3000
+    q, k, v = rand((nq, hq, d), dt, 7), rand((nk, hk, d), dt, 8), rand((nk, hk, d), dt, 9)
+    for at in (nk - 150, nk - 60, nk - 1):
+        k2, v2 = k.clone(), v.clone()
+        k2[at], v2[at] = what, what
+        out, lse = prompt_attention(q, k2, v2, starts([nq]), starts([nk]), return_lse=True)
+        blind = nq - (nk - at)  # the rows that do not see it
+        check_prompt(q[:blind], k[:at], v[:at], [blind], [at], True, out[:blind], lse[:blind])
+        assert not torch.isfinite(out[blind:].float()).any()
+
+
+def test_prompt_cut_in_a_graph():
+    say("prompt cut in a graph")
+    q, k, v = rand((40, 4, 128), BF16, 11), rand((6000, 2, 128), BF16, 12), rand((6000, 2, 128), BF16, 13)
+    cu, ck = starts([30, 10]), starts([2000, 4000])
+    out = torch.empty_like(q)
+    want = prompt_attention(q, k, v, cu, ck).clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        prompt_attention(q, k, v, cu, ck, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        prompt_attention(q, k, v, cu, ck, out=out)
+    for i in range(4):
+        q.copy_(rand(q.shape, BF16, 20 + i))
+        cu.copy_(starts([30 - 7 * i, 10 + 7 * i]) if i else starts([30, 10]))
+        cu[2] = 40
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, prompt_attention(q, k, v, cu, ck))
+    assert want.shape == out.shape
+
+
 @pytest.mark.parametrize("layout", ["fused", "head_major", "padded", "shared_row"])
 def test_prompt_strides(layout):
     hq, hk, d, lens = 4, 2, 128, [130, 64, 3]
