@@ -478,8 +478,9 @@ m2c_status m2c_ratio_search(m2c_layer* layer, const uint16_t* x, int32_t T, int3
  * multiple of n_kv_heads; with G = n_heads / n_kv_heads query head h reads
  * key/value head h / G. Rows of queries, keys, values and outputs are given by
  * two strides in elements, between tokens (head_dim .. 2^24) and between heads
- * (0 for keys or values that heads share); the head_dim elements of a head are
- * contiguous, and pointers and strides are multiples of 16 bytes (8 elements).
+ * (0 for rows that heads share; rows that are written must not overlap); the
+ * head_dim elements of a head are contiguous, and pointers and strides are
+ * multiples of 16 bytes (8 elements).
  *
  * Softmax statistics and sums are fp32; weights of the value product are
  * rounded to the 16-bit type of the matrix instruction that takes them. A
@@ -567,9 +568,11 @@ typedef struct {
 } m2c_kv_cache;
 
 /* seqs (in the calls below): dev int32 [n], the sequence of each row of the
- * call, no sequence twice; NULL means sequences 0 .. n - 1. A call that finds
- * an error on the device leaves that sequence as it was (attend and read give
- * zero rows) and sets a bit that m2c_kv_status reports. */
+ * call, no sequence twice; NULL means sequences 0 .. n - 1. What a call finds
+ * wrong on the device sets a bit that m2c_kv_status reports, and nothing out of
+ * range is touched: of a sequence out of range nothing is written but attend's
+ * zero row; an append that is refused leaves its sequence as it was; a block
+ * whose page is out of range is not stored, and is read and attended as zeros. */
 
 /* Forget the tokens of n sequences. */
 m2c_status m2c_kv_reset(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream);

@@ -85,6 +85,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
     starts (cu_k None: the same). causal: query i of lq sees keys 0 .. lk - lq
     + i of its sequence. max_q: longest query sequence if known (a hint
     for whether rows are split along their keys).
+    scale: of q.k, None or 0 for 1 / sqrt(head_dim).
     Returns out like q (contiguous unless given), or (out, lse) with lse fp32
     [total_q, n_heads] = ln sum exp(scale q.k)."""
     if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
@@ -230,7 +231,7 @@ class KVCache:
                stream=None):
         """Attention of one token per sequence, q [n, n_heads, head_dim], over
         all that sequence seqs[b] (default: b) holds. max_len: the longest of
-        them if known. track: add the blocks' attention weights to `weight`.
+        them if known. scale: as in prompt_attention. track: add the blocks' attention weights to `weight`.
         Returns out like q, or (out, lse) with lse fp32 [n, n_heads]."""
         if q.dim() != 3:
             _bad("q: need [n, n_heads, head_dim]")

@@ -54,6 +54,19 @@ m2c_status check_rows(const char* what, const void* p, const int64_t* stride, in
   return M2C_OK;
 }
 
+// Rows that are written: no two of them may overlap.
+m2c_status check_written(const char* what, const void* p, const int64_t* stride, int64_t tokens, int heads,
+                         int head_dim) {
+  const m2c_status rc = check_rows(what, p, stride, head_dim);
+  if (rc != M2C_OK) return rc;
+  if (stride[0] < (heads - 1) * stride[1] + head_dim && stride[1] < (tokens - 1) * stride[0] + head_dim)
+    return api_fail(M2C_ERR_INVALID_ARG, "%s: rows overlap with strides %lld, %lld", what,
+                    (long long)stride[0], (long long)stride[1]);
+  if (heads > 1 && stride[1] < head_dim)
+    return api_fail(M2C_ERR_INVALID_ARG, "%s: head stride %lld: need >= head_dim", what, (long long)stride[1]);
+  return M2C_OK;
+}
+
 m2c_status check_heads(int dtype, int n_heads, int n_kv_heads, int head_dim, float scale, int device) {
   if (dtype != M2C_DTYPE_FP16 && dtype != M2C_DTYPE_BF16)
     return api_fail(M2C_ERR_INVALID_ARG, "dtype %d: need M2C_DTYPE_FP16 or M2C_DTYPE_BF16", dtype);
@@ -152,7 +165,7 @@ m2c_status m2c_prompt_attention(const m2c_attn_desc* D, const void* q, const voi
                       (long long)need);
   }
   CHECKED(check_rows("q", q, D->q_stride, D->head_dim));
-  CHECKED(check_rows("out", out, D->out_stride, D->head_dim));
+  CHECKED(check_written("out", out, D->out_stride, total_q, D->n_heads, D->head_dim));
   if (total_k > 0) {
     CHECKED(check_rows("k", k, D->k_stride, D->head_dim));
     CHECKED(check_rows("v", v, D->v_stride, D->head_dim));
@@ -201,8 +214,8 @@ m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n
   if (total < 0 || total > kMaxRows)
     return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30]", (long long)total);
   if (total == 0) return M2C_OK;
-  CHECKED(check_rows("k", k, k_stride, C.head_dim));
-  CHECKED(check_rows("v", v, v_stride, C.head_dim));
+  CHECKED(check_written("k", k, k_stride, total, C.n_kv_heads, C.head_dim));
+  CHECKED(check_written("v", v, v_stride, total, C.n_kv_heads, C.head_dim));
   CurrentDevice g(cache->device);
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_read(C, seqs, n, cu, total, k, v, k_stride, v_stride,
@@ -233,7 +246,7 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
   if (track != 0 && track != 1) return api_fail(M2C_ERR_INVALID_ARG, "track %d: need 0 or 1", track);
   if (max_len < 0) return api_fail(M2C_ERR_INVALID_ARG, "max_len %d: need >= 0", max_len);
   CHECKED(check_rows("q", q, q_stride, C.head_dim));
-  CHECKED(check_rows("out", out, out_stride, C.head_dim));
+  CHECKED(check_written("out", out, out_stride, n, n_heads, C.head_dim));
   const int64_t need = m2c::kv_attend_workspace(C, n, n_heads, track, max_len);
   if (need > 0 && (!workspace || ((uintptr_t)workspace & 255)))
     return api_fail(M2C_ERR_INVALID_ARG, "workspace: need %lld bytes, 256-byte aligned", (long long)need);

@@ -99,6 +99,11 @@ def test_cache_refusals(lib, kw, needle):
     (lambda c: m2c.m2c_kv_attend(c, None, 1, 8, 0.0, P, (1024, 128), P, (1024, 128), None, 1, 64, None, 0, 0), m2c.M2C_ERR_INVALID_ARG, "workspace"),
     (lambda c: m2c.m2c_kv_attend(c, None, 1, 8, 0.0, P, (1024, 128), P, (1024, 128), None, 1, 64, P, 8, 0), m2c.M2C_ERR_CAPACITY, "workspace"),
     (lambda c: m2c.m2c_kv_attend(c, None, 1, 8, 0.0, P, (1024, 128), P, (1024, 128), None, 1, 64, P + 64, 1 << 30, 0), m2c.M2C_ERR_INVALID_ARG, "aligned"),
+    (lambda c: m2c.m2c_kv_attend(c, None, 2, 8, 0.0, P, (1024, 128), P, (1024, 0), None, 0, 64, None, 0, 0), m2c.M2C_ERR_INVALID_ARG, "out: "),
+    (lambda c: m2c.m2c_kv_attend(c, None, 2, 8, 0.0, P, (1024, 128), P, (512, 128), None, 0, 64, None, 0, 0), m2c.M2C_ERR_INVALID_ARG, "out: rows overlap"),
+    (lambda c: m2c.m2c_kv_attend(c, None, 2, 8, 0.0, P, (1024, 128), P, (1024, 64), None, 0, 64, None, 0, 0), m2c.M2C_ERR_INVALID_ARG, "out: head stride"),
+    (lambda c: m2c.m2c_kv_read(c, None, 1, P, 9, P, P, (256, 128), (128, 128), 0), m2c.M2C_ERR_INVALID_ARG, "v: rows overlap"),
+    (lambda c: m2c.m2c_kv_attend_workspace(c, 1, 8, 0, -1), m2c.M2C_ERR_INVALID_ARG, "max_len -1"),
     (lambda c: m2c.m2c_kv_evict(c, None, 1, 3, 2, 2, None, None, None, 0), m2c.M2C_ERR_INVALID_ARG, "keep 3"),
     (lambda c: m2c.m2c_kv_evict(c, None, 1, 3, -1, 2, None, None, None, 0), m2c.M2C_ERR_INVALID_ARG, "first -1"),
     (lambda c: m2c.m2c_kv_evict(c, None, 1, 3, 1, 2, P, None, None, 0), m2c.M2C_ERR_INVALID_ARG, "all three"),
