@@ -42,6 +42,13 @@ def _alloc(stream, device, *wanted):
         return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
 
 
+def _like(q, stream):
+    """An output like q, contiguous (the usual case by the shorter call)."""
+    if stream is None and q.is_contiguous():
+        return torch.empty_like(q)
+    return _alloc(stream, q.device, (q.shape, q.dtype))[0]
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -109,18 +116,10 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
         if len(_prompt_need) >= 4096:
             _prompt_need.clear()
         need = _prompt_need[key] = m2c.m2c_prompt_attention_workspace(desc, cu_q, cu_k, n, tq, k.shape[0])
-    want = []
-    if out is None:
-        want.append(((tq, hq, d), q.dtype))
-    if return_lse:
-        want.append(((tq, hq), torch.float32))
+    out = _like(q, stream) if out is None else out
+    lse = _alloc(stream, dev, ((tq, hq), torch.float32))[0] if return_lse else None
     if need:
-        want.append(((need,), torch.uint8))
-    got = iter(_alloc(stream, dev, *want))
-    out = next(got) if out is None else out
-    lse = next(got) if return_lse else None
-    if need:
-        work = next(got)
+        work, = _alloc(stream, dev, ((need,), torch.uint8))
         desc.workspace, desc.workspace_bytes = work.data_ptr(), need
     desc.out_stride = _rows("out", out, q.dtype, dev, hq, d)
     _check(m2c.load().m2c_prompt_attention(
@@ -245,19 +244,12 @@ class KVCache:
             if len(self._need) >= 4096:
                 self._need.clear()
             need = self._need[key] = m2c.m2c_kv_attend_workspace(self.desc, *key)
-        want = []
         if out is None:
-            want.append(((n, hq, self.head_dim), self.dtype))
+            out = _like(q, stream)
         elif out.shape != q.shape:
             _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
-        if return_lse:
-            want.append(((n, hq), torch.float32))
-        if need:
-            want.append(((need,), torch.uint8))
-        got = iter(_alloc(stream, self.device, *want))
-        out = next(got) if out is None else out
-        lse = next(got) if return_lse else None
-        work = next(got) if need else None
+        lse = _alloc(stream, self.device, ((n, hq), torch.float32))[0] if return_lse else None
+        work = _alloc(stream, self.device, ((need,), torch.uint8))[0] if need else None
         os = _rows("out", out, self.dtype, self.device, hq, self.head_dim)
         _check(self._lib.m2c_kv_attend(self.desc, _address(seqs), n, hq, 0.0 if scale is None else scale,
                                        q.data_ptr(), qs, out.data_ptr(), os, _address(lse), track,
