@@ -22,9 +22,9 @@
 // grid that runs at once; the lengths are on the device, so each workgroup finds
 // its share itself. A share may end inside a row: the parts of a row are joined
 // by a second launch. Within a share the four waves take the units in turn, each
-// with its own running m, l, O, joined through LDS. Calls whose rows alone fill
-// the GPU, or with more sequences than a wave has lanes, give each workgroup a
-// chunk of one row instead.
+// with its own running m, l, O, joined through LDS. Short rows are a workgroup's
+// each, which then adds the block weights too; rows between those, and calls with
+// more sequences than a wave has lanes, are cut into chunks (see split_of).
 //
 // Measured (kernel times): 131071 tokens of 8 heads of 128 (268 MB) 42 us, 6.4
 // TB/s with the Infinity Cache's share, and a join of 5; 32 sequences of 500 ..
@@ -56,6 +56,7 @@ struct AttendArgs {
   float c;
   int n, n_heads, group, tiles;  // tiles: head tiles of 16 per key/value head
   int splits, chunk;             // chunk: units per workgroup (where shares are not even)
+  int weigh_here;                // attend adds the block weights (a row is one workgroup's)
 };
 
 namespace {
@@ -115,13 +116,19 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t lo, uint32_t hi) {
 
 constexpr int kShares = 512;  // workgroups that run at once: two per CU
 
-// The even shares: lane b of a wave holds sequence b of the call, its rows' units
-// [start, start + cost * rows of a sequence) in the flat order.
+// What a row costs a workgroup beside its units, in units: queries, the first
+// loads' latency, the waves' join. (32 heads, 8 ragged sequences of up to 16000
+// tokens: 57 us with 1, 39 with 4, 36 with 8, 38 with 16.)
+constexpr int kRowCost = 8;
+
+// The even shares: lane b of a wave holds sequence b of the call, its rows'
+// [start, start + cost * rows of a sequence) in the flat order, each row's
+// kRowCost before its units.
 struct Shares {
   int s, len;           // sequence id (-1: no such), tokens
-  uint32_t cost, start; // units of a row (at least 1), first flat unit
+  uint32_t cost, start; // cost of a row, the first in the flat order
   uint32_t total;
-  int count;            // shares: share p is units [p total / count, (p + 1) total / count)
+  int count;            // shares: share p is [p total / count, (p + 1) total / count)
 
   __device__ __forceinline__ uint32_t first_of(int p) const {
     return (uint32_t)((uint64_t)p * total / count);
@@ -148,13 +155,28 @@ __device__ __forceinline__ Shares shares_of(const AttendArgs& A, int unit) {
       S.s = id;
       S.len = (int)clamp64(C.len[id], 0, (int64_t)C.max_blocks * C.block_tokens);
     }
-    S.cost = max(1, units_of(S.len, C.block_tokens, unit));
+    S.cost = kRowCost + units_of(S.len, C.block_tokens, unit);
   }
   const uint32_t all = S.cost * rows, incl = wave_incl_scan(all);
   S.start = incl - all;
   S.total = __builtin_amdgcn_readlane(incl, 63);
   S.count = min(kShares, max(A.n * rows, (int)(S.total / kWaves)));
   return S;
+}
+
+// Attention weight of a block: the sum over its units and the group's heads of
+// (sum of p) 2^(m of the unit - m) / l. fin: m and 1 / l of the group's heads.
+__device__ __forceinline__ float block_weight(const AttendArgs& A, int rk, int blk, int units, int per_block,
+                                              const float2* fin) {
+  float w = 0.0f;
+  for (int u = blk * per_block; u < min(units, (blk + 1) * per_block); ++u) {
+    const float2* p = A.wsum + ((int64_t)rk * A.C.max_blocks * per_block + u) * A.group;
+    for (int g = 0; g < A.group; ++g) {
+      const float m = fin[g].x == -INFINITY ? 0.0f : fin[g].x;
+      w += p[g].y * exp2_fast(p[g].x - m) * fin[g].y;
+    }
+  }
+  return w;
 }
 
 template <bool BF, int D, int UNIT, bool EVEN>
@@ -166,7 +188,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
   constexpr int VW = E / 4;      // code words of those
   constexpr int V2 = UNIT / 32;  // steps of the value product
   __shared__ __align__(16) float mrg[kWaves][16][D + 4];
-  __shared__ float2 mls[kWaves][16];
+  __shared__ float2 mls[kWaves][16], fins[16];
 
   const KvView& C = A.C;
   const int lane = threadIdx.x & 63, col = lane & 15, qr = lane >> 4;
@@ -193,10 +215,11 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
       s_id = __builtin_amdgcn_readlane(S.s, b);
       len = __builtin_amdgcn_readlane(S.len, b);
       rt = (int)(at / cost);
-      ua = (int)(at - rt * cost);
-      const uint32_t take = min(cost - ua, flat_end - flat);
+      const int in = (int)(at - rt * cost);
+      const uint32_t take = min(cost - in, flat_end - flat);
       whole = take == cost;
-      ub = min(ua + (int)take, units_of(len, BT, UNIT));
+      ua = max(0, in - kRowCost);
+      ub = max(0, in + (int)take - kRowCost);
       chunk = step = 64 * kWaves;
       part = (int64_t)b * rows + rt + blockIdx.x;  // a next row or a next share: one more
       flat += take;
@@ -488,7 +511,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
         for (int i = 0; i < E; i += 2) po[i / 2] = pack16<BF>(y[i] * inv, y[i + 1] * inv);
         if ((threadIdx.x & 15) == 0) {
           if (A.lse) A.lse[at] = (M - kLift + log2_fast(L)) * kLn2;
-          if (A.fin) A.fin[at] = make_float2(M, inv);
+          if (A.weigh_here) fins[hd] = make_float2(M, inv);
+          else if (A.fin) A.fin[at] = make_float2(M, inv);
         }
       } else {
         const int64_t at = part * min(A.group, 16) + hd;
@@ -498,7 +522,15 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
         for (int i = 0; i < E; i += 4) *(f32x4*)(po + i) = f32x4{y[i], y[i + 1], y[i + 2], y[i + 3]};
       }
     }
-    if (EVEN) __syncthreads();  // the next row writes the same LDS
+    if constexpr (EVEN) {
+      __syncthreads();  // the next row writes the same LDS
+    } else if (A.weigh_here) {
+      __syncthreads();
+      if (s_id < 0) return;
+      float* weight = C.weight + sh * C.max_blocks;
+      for (int blk = threadIdx.x; blk * BT < len; blk += kWaves * 64)
+        weight[blk] += block_weight(A, rk, blk, ub, halves + 1, fins);
+    }
   } while (EVEN && flat < flat_end);
 }
 
@@ -565,28 +597,19 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs A, int unit)
   }
 }
 
-// weight[s][h][block] += sum over the block's units and the group's heads of
-// (sum of p) 2^(m_unit - m) / l.
+// Adds the block weights where a row is not one workgroup's.
 __global__ void __launch_bounds__(256) weigh_kernel(const AttendArgs A, int unit, int parts) {
   const KvView& C = A.C;
-  const int per_block = C.block_tokens / unit;
-  const int rk = blockIdx.x / parts, part = blockIdx.x - rk * parts, b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
+  const int rk = blockIdx.x / parts, part = blockIdx.x - rk * parts;
+  const int b = rk / C.n_kv_heads, kvh = rk - b * C.n_kv_heads;
   const int s = A.seqs ? A.seqs[b] : b;
   if (s < 0 || s >= C.n_seqs) return;
   const int len = (int)clamp64(C.len[s], 0, (int64_t)C.max_blocks * C.block_tokens);
-  const int units = len / C.block_tokens * per_block + (len % C.block_tokens + unit - 1) / unit;
+  const int units = units_of(len, C.block_tokens, unit);
+  float* weight = C.weight + ((int64_t)s * C.n_kv_heads + kvh) * C.max_blocks;
   const float2* fin = A.fin + (int64_t)b * A.n_heads + kvh * A.group;
-  for (int blk = part * 256 + threadIdx.x; blk * C.block_tokens < len; blk += parts * 256) {
-    float w = 0.0f;
-    for (int u = blk * per_block; u < min(units, (blk + 1) * per_block); ++u) {
-      const float2* p = A.wsum + ((int64_t)rk * C.max_blocks * per_block + u) * A.group;
-      for (int g = 0; g < A.group; ++g) {
-        const float m = fin[g].x == -INFINITY ? 0.0f : fin[g].x;
-        w += p[g].y * exp2_fast(p[g].x - m) * fin[g].y;
-      }
-    }
-    C.weight[((int64_t)s * C.n_kv_heads + kvh) * C.max_blocks + blk] += w;
-  }
+  for (int blk = part * 256 + threadIdx.x; blk * C.block_tokens < len; blk += parts * 256)
+    weight[blk] += block_weight(A, rk, blk, units, C.block_tokens / unit, fin);
 }
 
 int unit_of(const KvView& C) { return C.block_tokens < 64 ? 32 : 64; }
@@ -607,21 +630,25 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   Split S;
   S.tiles = (group + 15) / 16;
   const int64_t rows = (int64_t)n * C.n_kv_heads * S.tiles;
-  // A row is left whole where it is four units, or where 256 rows of up to 32
-  // units are enough workgroups: the other half of the CU's waves would gain
-  // less than the join's launch takes (8 sequences of up to 2048 tokens x 32
-  // heads: 17.4 us and a join of 4 against 18.4). Else the shares are even where
-  // a wave can hold the sequences, and chunks of up to 32 units (16 where that
-  // is more than a round of workgroups) where there are more.
-  int64_t chunk = (rows * units + kShares - 1) / kShares;
-  if (chunk > 32) chunk = 16;
-  else if (rows >= 256 && units <= 32) chunk = units;
+  // Whole rows where they are short, the longer the more of them: the join's
+  // launch takes longer than what it saves (us whole and in parts: 8 rows of 13
+  // units 9.3 and 9.3, of 18 11.1 and 9.4; 64 rows of 24 13.3 and 13.5, of 32
+  // 16.6 and 14.4; 128 rows of 32 18.6 and 20.4).
+  const int64_t share = (rows * units + kShares - 1) / kShares;
+  int64_t chunk = share > 32 ? 16 : share;
+  if (units <= (rows >= 128 ? 32 : rows >= 64 ? 24 : 16)) chunk = units;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
   while ((units + chunk - 1) / chunk > kMaxSplits) chunk += kWaves;
   S.chunk = (int)chunk;
   S.splits = (int)((units + chunk - 1) / chunk);
   if (S.splits < 1) S.splits = 1;
-  S.even = S.splits > 1 && n <= 64 && rows * (cap / unit) < INT32_MAX;
+  // Else even shares, where they are long and a wave can hold the sequences, or
+  // chunks of a row of 4 to 32 units, 16 where that is more than a round of
+  // workgroups (shares and chunks: 8 ragged sequences of up to 20000 tokens x 32
+  // heads 74 and 83, x 8 heads of up to 16000 25 and 35, of up to 4000, 8 units a
+  // share, 15.6 and 16.3; 32 of one head of up to 4000, 4 a share, 12.3 and 12.1;
+  // 8 of 6000 each x 8 heads 26 and 24).
+  S.even = S.splits > 1 && share >= 8 && n <= 64 && rows * (cap / unit + kRowCost) < INT32_MAX;
   S.parts = S.splits == 1 ? 0 : S.even ? rows + kShares : rows * S.splits;
   return S;
 }
@@ -674,6 +701,7 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
     A.wsum = (float2*)ws;
   }
   const int unit = unit_of(C);
+  A.weigh_here = track && S.splits == 1 && S.tiles == 1;
   const int64_t grid = S.even ? kShares : (int64_t)n * C.n_kv_heads * S.tiles * S.splits;
   if (grid > INT32_MAX) return hipErrorInvalidValue;
   const auto launch = [&](auto bf, auto d, auto u, auto even) {
@@ -700,7 +728,7 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
   };
   hipError_t e = C.bf ? by_dim(std::true_type()) : by_dim(std::false_type());
   if (e != hipSuccess) return e;
-  if (track) {
+  if (track && !A.weigh_here) {
     const int64_t cap = (int64_t)C.max_blocks * C.block_tokens;
     const int64_t most = max_len > 0 && max_len < cap ? max_len : cap;
     const int64_t blocks = (most + C.block_tokens - 1) / C.block_tokens;

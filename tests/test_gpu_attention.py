@@ -700,6 +700,23 @@ def test_attend_many_ragged_sequences(n):
         check_attend(c, q, o, e, list(range(n)))
 
 
+@pytest.mark.parametrize("hq,hk,d,dt", [(16, 8, 128, BF16), (32, 8, 64, F16)])
+def test_attend_however_it_is_split(hq, hk, d, dt):
+    """Whole rows, chunks and even shares by the longest length the caller
+    names: the same values and block weights; rows without tokens, of one and of
+    many between long ones."""
+    say(f"attend splits {hq}/{hk}x{d} {dt}")
+    lens = [4000, 0, 1, 700, 64, 65, 0, 3333, 128, 2, 1999, 63]
+    c = filled(lens, hk, d, 64, dt, 64, 119)
+    q = rand((len(lens), hq, d), dt, 122, 1.5)
+    for hint in (4000, 2000, 1500, 64, 0):
+        before = c.weight.clone()
+        out, lse = c.attend(q, max_len=hint, track=True, return_lse=True)
+        c.check()
+        check_attend(c, q, out, lse, list(range(len(lens))), before=before)
+        assert bool((out[[1, 6]] == 0).all()) and bool((c.weight[[1, 6]] == before[[1, 6]]).all())
+
+
 def test_attend_rows_strides_and_scale():
     say("attend subset, strides, scale")
     c = filled([70, 0, 500, 64, 129], 2, 128, 64, BF16, 9, 120)
