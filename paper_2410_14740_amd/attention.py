@@ -105,26 +105,31 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
         _bad("cu_q: need the row starts of at least one sequence and the end")
     _ints("cu_q", cu_q, n + 1, dev)
     cu_k = cu_q if cu_k is None else _ints("cu_k", cu_k, n + 1, dev)
-    strides = [_rows(name, t, q.dtype, dev, h, d) for name, t, h in (("q", q, hq), ("k", k, hk), ("v", v, hk))]
-    if out is not None and out.shape != q.shape:
+    dt, tk = q.dtype, k.shape[0]
+    if out is None:
+        out, out_strides = _like(q, stream), _I64x2(hq * d, d)
+    elif out.shape != q.shape:
         _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
-    desc = m2c.AttnDesc(_DTYPES[q.dtype], hq, hk, d, 1 if causal else 0, dev.index,
-                        0.0 if scale is None else scale, max_q, *strides)
-    key = (hq, hk, d, n, tq, k.shape[0], max_q, cu_q.data_ptr() == cu_k.data_ptr())
+    else:
+        out_strides = _rows("out", out, dt, dev, hq, d)
+    lse = _alloc(stream, dev, ((tq, hq), torch.float32))[0] if return_lse else None
+    desc = m2c.AttnDesc(_DTYPES[dt], hq, hk, d, 1 if causal else 0, dev.index,
+                        0.0 if scale is None else scale, max_q, _rows("q", q, dt, dev, hq, d),
+                        _rows("k", k, dt, dev, hk, d), _rows("v", v, dt, dev, hk, d),
+                        out_strides)
+    starts, key_starts = cu_q.data_ptr(), cu_k.data_ptr()
+    key = (n, tq, tk, max_q, hq, hk, d, starts == key_starts)
     need = _prompt_need.get(key)
     if need is None:
         if len(_prompt_need) >= 4096:
             _prompt_need.clear()
-        need = _prompt_need[key] = m2c.m2c_prompt_attention_workspace(desc, cu_q, cu_k, n, tq, k.shape[0])
-    out = _like(q, stream) if out is None else out
-    lse = _alloc(stream, dev, ((tq, hq), torch.float32))[0] if return_lse else None
+        need = _prompt_need[key] = m2c.m2c_prompt_attention_workspace(desc, cu_q, cu_k, n, tq, tk)
     if need:
         work, = _alloc(stream, dev, ((need,), torch.uint8))
         desc.workspace, desc.workspace_bytes = work.data_ptr(), need
-    desc.out_stride = _rows("out", out, q.dtype, dev, hq, d)
     _check(m2c.load().m2c_prompt_attention(
-        desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, tq,
-        k.shape[0], out.data_ptr(), _address(lse), _raw(stream, dev)))
+        desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), starts, key_starts, n, tq, tk, out.data_ptr(),
+        _address(lse), _raw(stream, dev)))
     return (out, lse) if return_lse else out
 
 
@@ -245,12 +250,13 @@ class KVCache:
                 self._need.clear()
             need = self._need[key] = m2c.m2c_kv_attend_workspace(self.desc, *key)
         if out is None:
-            out = _like(q, stream)
+            out, os = _like(q, stream), _I64x2(hq * self.head_dim, self.head_dim)
         elif out.shape != q.shape:
             _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+        else:
+            os = _rows("out", out, self.dtype, self.device, hq, self.head_dim)
         lse = _alloc(stream, self.device, ((n, hq), torch.float32))[0] if return_lse else None
         work = _alloc(stream, self.device, ((need,), torch.uint8))[0] if need else None
-        os = _rows("out", out, self.dtype, self.device, hq, self.head_dim)
         _check(self._lib.m2c_kv_attend(self.desc, _address(seqs), n, hq, 0.0 if scale is None else scale,
                                        q.data_ptr(), qs, out.data_ptr(), os, _address(lse), track,
                                        max_len, _address(work), need, _raw(stream, self.device)))

@@ -49,6 +49,7 @@ struct PromptArgs {
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // bytes
   float* part_o;    // [2 extra][units][kRows][D] unnormalized outputs of parts of rows
   float2* part_ml;  // [2 extra][units][kRows] their m and l
+  int32_t* cut;     // whether any row tile is cut
   float c;          // scale * log2 e
   int n_seqs, n_heads, causal;
   int pack;    // query heads of a key/value head whose rows lie in one tile: all, or 1
@@ -226,6 +227,7 @@ struct Plan {
   int rows, keyed, per, start;
   int row_start, slot_start;  // its first among the row tiles and parts of the sequences that are cut
   int most;
+  bool any;
 };
 
 __device__ __forceinline__ Plan plan_of(const PromptArgs& A) {
@@ -261,7 +263,9 @@ __device__ __forceinline__ Plan plan_of(const PromptArgs& A) {
     P.per = P.keyed > 0 ? (kt + P.most - 1) / P.most : 1;
     cut = P.per > 1 ? P.keyed * P.per : 0;
     const uint32_t extra = P.per > 1 ? (uint32_t)(cut - P.keyed) : 0u;
-    if (__builtin_amdgcn_readlane(wave_incl_scan(extra), 63) <= A.extra) break;
+    const int all = __builtin_amdgcn_readlane(wave_incl_scan(extra), 63);
+    P.any = all > 0;
+    if (all <= A.extra) break;
   }
   const int items = P.per > 1 ? cut + P.rows - P.keyed : P.rows;
   const int cut_rows = P.per > 1 ? P.keyed : 0;
@@ -300,6 +304,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) prompt_attention_kernel(const 
   int qt, b, part = 0, most = 0, slot = 0;
   if constexpr (SPLIT) {
     const Plan P = plan_of(A);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *A.cut = P.any;
     const int items = P.per > 1 ? P.keyed * P.per + P.rows - P.keyed : P.rows;
     const unsigned long long own = __ballot(x >= P.start && x < P.start + items);
     if (!own) return;
@@ -578,6 +583,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) prompt_attention_kernel(const 
 template <bool BF, int D>
 __global__ void __launch_bounds__(kWaves * 64) prompt_join_kernel(const PromptArgs A) {
   constexpr int DT = D / 32;
+  if (!*A.cut) return;
   const Plan P = plan_of(A);
   for (int id = blockIdx.x;; id += gridDim.x) {  // ends past the row tiles that were cut
     const int x = id / (A.units * DT), r = id - x * (A.units * DT);
@@ -683,7 +689,7 @@ hipError_t launch_rows(PromptArgs& A, hipStream_t stream) {
 int64_t prompt_workspace(const m2c_attn_desc* D, bool self, int n_seqs, int64_t total_q, int64_t total_k) {
   const int64_t parts = 2 * (int64_t)extra_of(D, self, n_seqs, total_q, total_k) *
                         (D->n_heads / pack_of(D, total_q));
-  return round256(parts * kRows * 8) + parts * kRows * D->head_dim * 4;
+  return parts ? 256 + round256(parts * kRows * 8) + parts * kRows * D->head_dim * 4 : 0;
 }
 
 hipError_t launch_prompt_attention(const m2c_attn_desc* D, const void* q, const void* k,
@@ -712,8 +718,10 @@ hipError_t launch_prompt_attention(const m2c_attn_desc* D, const void* q, const 
   A.shared = A.units / D->n_kv_heads;
   A.causal = D->causal;
   A.extra = D->workspace ? extra_of(D, cu_q == cu_k, n_seqs, total_q, total_k) : 0;
-  A.part_ml = (float2*)D->workspace;
-  A.part_o = (float*)((uint8_t*)D->workspace + round256(2 * (int64_t)A.extra * A.units * kRows * 8));
+  uint8_t* ws = (uint8_t*)D->workspace;
+  A.cut = (int32_t*)ws;
+  A.part_ml = (float2*)(ws + 256);
+  A.part_o = (float*)(ws + 256 + round256(2 * (int64_t)A.extra * A.units * kRows * 8));
   if (D->dtype == M2C_DTYPE_BF16)
     return D->head_dim == 128 ? launch_rows<true, 128>(A, stream) : launch_rows<true, 64>(A, stream);
   return D->head_dim == 128 ? launch_rows<false, 128>(A, stream) : launch_rows<false, 64>(A, stream);
