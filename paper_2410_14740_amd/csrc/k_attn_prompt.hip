@@ -82,17 +82,17 @@ __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes) {
 }
 
 // 16 bytes per lane from buffer offset `off` (per lane) straight into LDS (lane
-// i's land at dst + 16 i, dst the same in every lane). Written out so that the
+// i's land at dst + 16 i, dst the same in every lane, in m0, which is an operand
+// so that the compiler knows what it holds). Written out so that the
 // compiler does not wait for it at every LDS read that follows: the loads of
 // one tile run while the tile before it is used, and one explicit wait and a
 // barrier stand between the two.
 __device__ __forceinline__ void load_lds16(u32x4 buf, uint32_t off, uint32_t dst) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
       "s_nop 0\n\t"
       "buffer_load_dwordx4 %1, %0, 0 offen lds"
       :
-      : "s"(buf), "v"(off), "s"(dst)
+      : "s"(buf), "v"(off), "{m0}"(dst)
       : "memory");
 }
 
