@@ -274,7 +274,9 @@ __global__ void __launch_bounds__(kWaves * 64, 2) attend_kernel(const AttendArgs
       big = max(big, (uint32_t)__shfl_xor((int)big, 16));
       big = max(big, (uint32_t)__shfl_xor((int)big, 32));
       const int ex = big >= 0x80u ? (int)(big >> 7) - 127 : big ? -126 : 14;  // the largest is below 2^(ex + 1)
-      const int up = 14 - ex;
+      // By 2^116 at most: every bf16 number is a multiple of 2^-133, so all are
+      // exact then, and c 2^-up keeps its bits (scales of 2^-10 and more).
+      const int up = min(14 - ex, 116);
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
