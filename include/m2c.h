@@ -521,8 +521,9 @@ int64_t m2c_prompt_attention_workspace(const m2c_attn_desc* desc, const int32_t*
  *               [0, total_k]; they may be the same array
  *   q, out      dev [total_q] rows;  k, v  dev [total_k] rows
  *   lse         dev fp32 [total_q][n_heads], ln sum exp(scale <q, k>), or NULL
- * Output rows of no sequence are not written. Results are the same bits on
- * every run with the same arguments. */
+ * Output rows of no sequence are not written. With starts that do not ascend
+ * nothing outside the arrays is touched, but which rows are computed is not
+ * defined. Results are the same bits on every run with the same arguments. */
 m2c_status m2c_prompt_attention(const m2c_attn_desc* desc, const void* q, const void* k,
                                 const void* v, const int32_t* cu_q, const int32_t* cu_k,
                                 int32_t n_seqs, int64_t total_q, int64_t total_k, void* out,
@@ -572,7 +573,9 @@ typedef struct {
  * wrong on the device sets a bit that m2c_kv_status reports, and nothing out of
  * range is touched: of a sequence out of range nothing is written but attend's
  * zero row; an append that is refused leaves its sequence as it was; a block
- * whose page is out of range is not stored, and is read and attended as zeros. */
+ * whose page is out of range is not stored, and is read and attended as zeros.
+ * Row starts that do not ascend are reported and touch nothing out of range, but
+ * which rows the sequences of the call then get is not defined. */
 
 /* Forget the tokens of n sequences. */
 m2c_status m2c_kv_reset(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream);
@@ -639,7 +642,7 @@ m2c_status m2c_kv_evict(const m2c_kv_cache* cache, const int32_t* seqs, int32_t 
 
 /* Waits for `stream`, then reports and clears what the calls above found on
  * the device since the last check: M2C_ERR_INVALID_ARG (a sequence or page out
- * of range), M2C_ERR_CAPACITY, M2C_ERR_STATE, or M2C_OK. */
+ * of range, row starts that do not ascend), M2C_ERR_CAPACITY, M2C_ERR_STATE, or M2C_OK. */
 m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream);
 
 /* Test support. Copies one record of the host store (no device work). */

@@ -280,5 +280,6 @@ class KVCache:
 
     def check(self, stream=None):
         """Wait for `stream`; raise what the calls so far found on the device
-        (a sequence or page out of range, a full sequence, a bad place)."""
+        (a sequence or page out of range, row starts that do not ascend, a full
+        sequence, a bad place)."""
         _check(self._lib.m2c_kv_status(self.desc, _raw(stream, self.device)))

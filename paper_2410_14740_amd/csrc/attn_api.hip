@@ -296,7 +296,8 @@ m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream) {
     return api_fail(M2C_ERR_HIP, "cache status: %s", hipGetErrorString(e));
   }
   if (bits & m2c::kKvBadIndex)
-    return api_fail(M2C_ERR_INVALID_ARG, "a call used a sequence or page id out of range (status 0x%x)", bits);
+    return api_fail(M2C_ERR_INVALID_ARG, "a call used a sequence or page id out of range, or row starts that "
+                    "do not ascend (status 0x%x)", bits);
   if (bits & m2c::kKvCapacity)
     return api_fail(M2C_ERR_CAPACITY, "an append would have passed max_blocks * block_tokens tokens; "
                     "the sequence was left as it was (status 0x%x)", bits);

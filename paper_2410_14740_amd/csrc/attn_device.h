@@ -97,7 +97,8 @@ __device__ __forceinline__ int64_t item_start(int64_t cu, int b, int per, int mo
   return cu * mul / per + (int64_t)b * more;
 }
 
-// The sequence that owns item x, or -1 (wave-uniform).
+// The sequence that owns item x, or -1 (wave-uniform). Where cu does not ascend
+// x may lie before the first item of the one that this names.
 __device__ __forceinline__ int find_item(const int32_t* cu, int n, int64_t total, int64_t x,
                                          int per, int more, int mul = 1) {
   const int lane = threadIdx.x & 63;

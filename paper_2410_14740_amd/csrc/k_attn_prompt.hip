@@ -207,7 +207,7 @@ __device__ __forceinline__ int find_tile(const PromptArgs& A, int x, int* qt) {
     const int64_t lo = clamp64(A.cu_q[b], 0, A.total_q), hi = clamp64(A.cu_q[b + 1], lo, A.total_q);
     tiles = ((int)(hi - lo) * A.pack + kRows - 1) / kRows;
     j = x - (int)item_start(lo, b, kRows, 1, A.pack);
-    if (j >= tiles) return -1;
+    if (j < 0 || j >= tiles) return -1;  // below 0: starts that do not ascend
   }
   *qt = A.causal ? tiles - 1 - j : j;
   return b;

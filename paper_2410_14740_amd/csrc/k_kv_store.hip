@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
     const int64_t s0 = item_start(row0, b, BT, 2);
     item = (int)(x - s0);
     items = (int)(item_start(row1, b + 1, BT, 2) - s0);
-    if (item >= items) return;  // past the last sequence's
+    if (item < 0 || item >= items) return;  // past the last sequence's, or starts that do not ascend
   }
   if (nb == 0) return;  // nothing of this sequence changes
   const int s = seqs ? seqs[b] : b;
@@ -217,6 +217,7 @@ __global__ void __launch_bounds__(256) length_kernel(const KvView C, const int32
                                                      const int32_t* pos) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   if (b >= n) return;
+  if (cu[b + 1] < cu[b]) atomicOr(C.status, kKvBadIndex);
   const int64_t row0 = clamp64(cu[b], 0, total);
   const int nb = (int)(clamp64(cu[b + 1], row0, total) - row0);
   const int s = seqs ? seqs[b] : b;
@@ -233,10 +234,13 @@ __global__ void __launch_bounds__(256) read_kernel(const KvView C, const int32_t
   constexpr int CH = D / 8, TP = 256 / CH;
   constexpr int NP = BT / TP;
   const int x = blockIdx.x / C.n_kv_heads, head = blockIdx.x - x * C.n_kv_heads, tid = threadIdx.x;
+  // there are n workgroups or more
+  if (tid == 0 && (int)blockIdx.x < n && cu[blockIdx.x + 1] < cu[blockIdx.x]) atomicOr(C.status, kKvBadIndex);
   const int b = find_item(cu, n, total, x, BT, 1);
   if (b < 0) return;
   const int64_t row0 = clamp64(cu[b], 0, total), row1 = clamp64(cu[b + 1], row0, total);
   const int blk = (int)(x - item_start(row0, b, BT, 1));
+  if (blk < 0) return;  // starts that do not ascend
   const int s = seqs ? seqs[b] : b;
   if (s < 0 || s >= C.n_seqs) {
     if (tid == 0) atomicOr(C.status, kKvBadIndex);

@@ -8,7 +8,7 @@
 namespace m2c {
 
 // Bits of the cache's status word, reported (and cleared) by m2c_kv_status.
-constexpr int kKvBadIndex = 1;  // a sequence id or a live page id out of range
+constexpr int kKvBadIndex = 1;  // a sequence id or a live page id out of range, row starts that do not ascend
 constexpr int kKvCapacity = 2;  // an append past max_blocks
 constexpr int kKvState = 4;     // an append at a place that is no place of the sequence
 

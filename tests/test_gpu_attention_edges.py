@@ -1,9 +1,11 @@
 """Edges of the attention calls. The bounds are those of test_gpu_attention.py."""
 import pytest
+import torch
 
 from helpers import say
-from paper_2410_14740_amd.attention import KVCache
-from test_gpu_attention import BF16, check_attend, rand, starts
+from paper_2410_14740_amd import m2c
+from paper_2410_14740_amd.attention import KVCache, prompt_attention
+from test_gpu_attention import BF16, F16, check_attend, rand, starts
 
 pytestmark = pytest.mark.gpu
 
@@ -19,3 +21,76 @@ def test_attend_tiny_queries(qs, ks, scale, n):
     q = rand((1, 6, 64), BF16, 303, qs)
     out, lse = c.attend(q, scale=scale, return_lse=True)
     check_attend(c, q, out, lse, [0], scale=scale)
+
+
+def item_before_the_first(cu, per, more, total):
+    """Some work item of packed sequences falls before the first item of the
+    sequence that a count of the starts at or before it names."""
+    first = [c // per + b * more for b, c in enumerate(cu[:-1])]
+    for x in range(total // per + (len(cu) - 1) * more):
+        b = sum(f <= x for f in first) - 1
+        if b >= 0 and x < first[b] and cu[b + 1] > cu[b]:
+            return True
+    return False
+
+
+BACKWARDS = [[0, 1000, 1100, 10, 20], [5, 1000, 1064, 0, 300, 20], [64, 900, 1000, 3, 1100, 2]]
+
+
+@pytest.mark.parametrize("cu", BACKWARDS)
+def test_starts_that_do_not_ascend_stay_in_range(cu):
+    """They are the caller's mistake: the call says so, and touches no other
+    sequence's page, tail, weight or length and no row outside its arrays."""
+    say(f"starts that do not ascend {cu}")
+    H, d, B, T, n = 2, 64, 64, 1100, len(cu) - 1
+    assert item_before_the_first(cu, B, 2, T) and item_before_the_first(cu, B, 1, T)
+    starts_ = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    seqs = torch.tensor([1, 3, 5, 7, 9][:n], dtype=torch.int32, device="cuda")
+    others = [0, 2, 4, 6, 8, 10] + [9] * (n < 5)
+    c = KVCache(11, H, d, 20, block_tokens=B)
+    c.append(rand((11 * 70, H, d), F16, 310), rand((11 * 70, H, d), F16, 311), cu=starts([70] * 11))
+    c.check()
+    c.weight.fill_(3.0)
+    pages = c.table[others].long()
+
+    def held():
+        rows = {"table": c.table, **{name: getattr(c, name)[others] for name in ("len", "weight", "tail_k", "tail_v")},
+                **{name: getattr(c, name)[pages] for name in ("k_codes", "v_codes", "k_scale", "v_scale")}}
+        return {name: t.contiguous().view(torch.uint8).clone() for name, t in rows.items()}  # unused places hold anything
+
+    def same():
+        now = held()
+        return all(torch.equal(now[name], before[name]) for name in now)
+
+    before = held()
+    room = rand((T + 400, H, d), F16, 312)
+    c.append(room[200:200 + T], room[200:200 + T], cu=starts_, seqs=seqs)
+    with pytest.raises(m2c.M2CError) as e:
+        c.check()
+    assert e.value.status == m2c.M2C_ERR_INVALID_ARG and "ascend" in str(e.value)
+    assert same()
+    k, v = (torch.full((T + 4000, H, d), 9.0, dtype=F16, device="cuda") for _ in range(2))
+    c.read(starts_, seqs=seqs, k=k[2000:2000 + T], v=v[2000:2000 + T])
+    with pytest.raises(m2c.M2CError) as e:
+        c.check()
+    assert e.value.status == m2c.M2C_ERR_INVALID_ARG and "ascend" in str(e.value)
+    for t in (k, v):
+        assert bool((t[:2000] == 9).all()) and bool((t[2000 + T:] == 9).all())
+    assert same()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("many", [False, True])
+def test_prompt_starts_that_do_not_ascend_stay_in_range(many, causal):
+    say(f"prompt starts that do not ascend {many} {causal}")
+    hq, d, T = 2, 64, 3000
+    cu = [0, 2000, 2500, 10, 20] if not many else [0, 2000, 2500, 10, 20] + [20 + 7 * i for i in range(80)]
+    assert item_before_the_first([2 * c for c in cu], 128, 1, 2 * T)
+    room = torch.full((T + 8000, hq, d), 9.0, dtype=F16, device="cuda")
+    x = torch.zeros((T + 8000, hq, d), dtype=F16, device="cuda")
+    q = x[4000:4000 + T]
+    starts_ = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    for cu_k in (starts_, torch.zeros_like(starts_)):
+        prompt_attention(q, q[:, :1], q[:, :1], starts_, cu_k, causal=causal, out=room[4000:4000 + T])
+        torch.cuda.synchronize()
+        assert bool((room[:4000] == 9).all()) and bool((room[4000 + T:] == 9).all())
