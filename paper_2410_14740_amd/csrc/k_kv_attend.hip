@@ -646,8 +646,6 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendArgs A, int unit,
 
 int unit_of(const KvView& C) { return C.block_tokens < 64 ? 32 : 64; }
 
-constexpr int kMaxSplits = 1024;
-
 struct Split {
   int tiles, splits, chunk;
   bool even;
@@ -667,21 +665,28 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   // units 9.3 and 9.3, of 18 11.1 and 9.4; 64 rows of 24 13.3 and 13.5, of 32
   // 16.6 and 14.4; 128 rows of 32 18.6 and 20.4).
   const int64_t share = (rows * units + kShares - 1) / kShares;
-  int64_t chunk = share > 32 ? 16 : share;
-  if (units <= (rows >= 128 ? 32 : rows >= 64 ? 24 : 16)) chunk = units;
-  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
-  while ((units + chunk - 1) / chunk > kMaxSplits) chunk += kWaves;
-  S.chunk = (int)chunk;
-  S.splits = (int)((units + chunk - 1) / chunk);
-  if (S.splits < 1) S.splits = 1;
+  const bool whole = units <= (rows >= 128 ? 32 : rows >= 64 ? 24 : 16);
   // Else even shares, where they are long and a wave can hold the sequences, or
-  // chunks of a row of 4 to 32 units, 16 where that is more than a round of
-  // workgroups (shares and chunks: 8 ragged sequences of up to 20000 tokens x 32
+  // chunks of a row of 4 to 32 units, 16 and more where that is more than a round
+  // of workgroups (shares and chunks: 8 ragged sequences of up to 20000 tokens x 32
   // heads 74 and 83, x 8 heads of up to 16000 25 and 35, of up to 4000, 8 units a
   // share, 15.6 and 16.3; 32 of one head of up to 4000, 4 a share, 12.3 and 12.1;
   // 8 of 6000 each x 8 heads 26 and 24).
-  S.even = S.splits > 1 && share >= 8 && n <= 64 && rows * (cap / unit + kRowCost) < INT32_MAX;
-  S.parts = S.splits == 1 ? 0 : S.even ? rows + kShares : rows * S.splits;
+  S.even = !whole && share >= 8 && n <= 64 && rows * (cap / unit + kRowCost) < INT32_MAX;
+  // With chunks of 16 for any number of rows the parts would grow with the longest
+  // length that the caller allows. So there are at most kRounds rounds of
+  // them, and the rows' number of parts is odd, so that the first parts, all that
+  // short rows have, fall on every XCD (us and MB of workspace with chunks of 16 and
+  // so, 64 / 8 heads: 96 ragged sequences of up to 16000 tokens 407, 51 and 311, 35;
+  // one of 100000 among 127 short ones 246, 417 and 180, 38; 128 of up to 2000 where
+  // 131072 are allowed 256, 550 and 82, 38; 1100 of up to 2100 622, 110 and 437, 0).
+  constexpr int kRounds = 16;
+  int64_t chunk = whole ? units : share > 32 ? std::max<int64_t>(16, (share + kRounds - 1) / kRounds) : share;
+  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+  S.splits = (int)((units + chunk - 1) / chunk);
+  if (share > 32 && !whole) S.splits |= 1;
+  S.chunk = (int)std::min<int64_t>(chunk, 64 * kWaves);  // a lane holds one page of a wave's
+  S.parts = S.even ? rows + kShares : S.splits == 1 ? 0 : rows * S.splits;
   return S;
 }
 
@@ -733,7 +738,7 @@ hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_h
     A.wsum = (float2*)ws;
   }
   const int unit = unit_of(C);
-  A.weigh_here = track && S.splits == 1 && S.tiles == 1;
+  A.weigh_here = track && !S.parts && S.tiles == 1;
   A.whole_fin = S.even || !S.parts;
   const int64_t grid = S.even ? kShares : (int64_t)n * C.n_kv_heads * S.tiles * S.splits;
   const int64_t cap = (int64_t)C.max_blocks * C.block_tokens;

@@ -137,6 +137,17 @@ def test_workspace_sizes(lib):
     assert ws(1, 1, 64) >= 8 * 16384 * 8
 
 
+@pytest.mark.parametrize("max_blocks", [300, 2048, 16384])
+def test_workspace_of_many_sequences(lib, max_blocks):
+    """Parts of rows, each 8 heads of 128 sums with m and l: at most 16 rounds of
+    512 workgroups and two a row, however long a sequence may get."""
+    for n in (64, 65, 128, 1000, 65535):
+        c = cache(n_seqs=n, n_kv_heads=8, max_blocks=max_blocks)
+        for most in (0, 5000):
+            need = m2c.m2c_kv_attend_workspace(c, n, 64, 0, most)
+            assert need <= (16 * 512 + 2 * 8 * n) * 8 * (128 * 4 + 8) + 512, (n, most)
+
+
 def test_prompt_workspace(lib):
     """Room for parts of rows where some may see many more keys than others."""
     need = lambda d, same, n, tq, tk: m2c.m2c_prompt_attention_workspace(d, P, P if same else 2 * P, n, tq, tk)  # noqa: E731

@@ -94,3 +94,36 @@ def test_prompt_starts_that_do_not_ascend_stay_in_range(many, causal):
         prompt_attention(q, q[:, :1], q[:, :1], starts_, cu_k, causal=causal, out=room[4000:4000 + T])
         torch.cuda.synchronize()
         assert bool((room[:4000] == 9).all()) and bool((room[4000 + T:] == 9).all())
+
+
+@pytest.mark.parametrize("n,hq,hk,d,dt,longest,hints", [
+    (70, 16, 8, 64, F16, 9000, (9000, 0)),      # chunks of 16 units
+    (66, 8, 8, 128, BF16, 30000, (30000,)),     # larger ones
+    (65, 40, 2, 64, BF16, 20000, (20000, 700)),  # two tiles of heads, a hint far too short
+    (66, 128, 128, 64, F16, 16500, (16500,)),   # whole rows of more units than a wave's lanes hold at once
+])
+def test_attend_more_sequences_than_lanes(n, hq, hk, d, dt, longest, hints):
+    say(f"attend {n} sequences {hq}/{hk}x{d} {dt} up to {longest}")
+    lens = [(53 * i) % 200 if i % 5 else i % 3 for i in range(n)]
+    lens[n // 2], lens[n - 2] = longest, longest // 3
+    if hk == 128:
+        lens = [min(x, 70) for x in lens]
+        lens[n // 2] = longest
+    c = KVCache(n, hk, d, longest // 64 + 2, dtype=dt, n_pages=sum(x // 64 for x in lens) * hk + 1)
+    pages = torch.randperm(c.k_codes.shape[0], generator=torch.Generator().manual_seed(320)).int().cuda()
+    c.table.fill_(-1)
+    at = 0
+    for b, x in enumerate(lens):
+        c.table[b, :, :x // 64] = pages[at:at + x // 64 * hk].view(hk, x // 64)
+        at += x // 64 * hk
+    c.append(rand((sum(lens), hk, d), dt, 321), rand((sum(lens), hk, d), dt, 322), cu=starts(lens))
+    q = rand((n, hq, d), dt, 323, 1.5)
+    some = sorted({0, 1, 5, n // 2, n // 2 + 1, n - 2, n - 1})
+    for hint in hints:
+        for track in (False, True):
+            before = c.weight.clone()
+            out, lse = c.attend(q, max_len=hint, track=track, return_lse=True)
+            c.check()
+            check_attend(c, q[some], out[some], lse[some], some, before=before if track else None)
+            assert track or torch.equal(c.weight, before)
+            assert bool((out[[i for i, x in enumerate(lens) if x == 0]] == 0).all())
