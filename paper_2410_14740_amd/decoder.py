@@ -53,6 +53,8 @@ class DecoderLayer:
 
     def __init__(self, ffn, k, n16, n8, n_seqs, n_heads, n_kv_heads, max_tokens, weights,
                  block_tokens=64, budget=0):
+        if budget < 0:
+            raise ValueError(f"budget {budget}: need a number of blocks, or 0 for no limit")
         d = ffn.desc.d_model
         self.ffn, self.k, self.n16, self.n8, self.step = ffn, k, n16, n8, 0
         self.n_heads, self.n_kv_heads, self.dim = n_heads, n_kv_heads, d // n_heads
@@ -108,7 +110,10 @@ class DecoderLayer:
         self.feed_forward(x)
 
     def evict(self, first=1, recent=2):
-        self.cache.evict(self.budget, first, recent)
+        """Blocks beyond the budget leave, not the first `first` and the last
+        `recent` of those that may (as many as the budget holds)."""
+        first = min(first, self.budget)
+        self.cache.evict(self.budget, first, min(recent, self.budget - first))
 
 
 def _starts(lens):

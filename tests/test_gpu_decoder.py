@@ -118,3 +118,15 @@ def test_decode_with_a_budget():
     # without a limit nothing leaves, and the two agree up to the first eviction
     free, _ = decoder.run(stack(2, 512, block=block), prompts(lens), 1, chunk=128)
     assert off(rows[0], free[0]) <= 1e-3
+
+
+@pytest.mark.parametrize("budget", [1, 2])
+def test_decode_with_a_small_budget(budget):
+    """Budgets below the blocks that an eviction spares by itself."""
+    say(f"decoder with a budget of {budget}")
+    lens, steps, block = [130, 40], 100, 32
+    layers = stack(2, 256, layers=1, budget=budget, block=block)
+    rows, held = decoder.run(layers, prompts(lens), steps, chunk=128)
+    assert bool(torch.isfinite(rows).all())
+    for n, m in zip(held, lens):
+        assert (n - 1) // block <= budget and (n - m - steps) % block == 0 and n < m + steps
