@@ -140,6 +140,8 @@ def run(layers, prompts, tokens, chunk=256):
     the decoded rows [tokens][sequences][d] and the sequences' lengths in the
     cache."""
     n = len(prompts)
+    if any(p.shape[0] == 0 for p in prompts):
+        raise ValueError("a prompt without tokens: decoding starts from a prompt's last row")
     done, last = [0] * n, [None] * n
     while any(done[b] < prompts[b].shape[0] for b in range(n)):
         lens = [min(chunk, prompts[b].shape[0] - done[b]) for b in range(n)]
@@ -170,13 +172,15 @@ def run(layers, prompts, tokens, chunk=256):
     return torch.stack(rows) if rows else x[None][:0], layers[0].cache.len.cpu().tolist()
 
 
-def main():
+def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--prompt", default="700,90,333", help="prompt lengths")
     ap.add_argument("--tokens", type=int, default=64)
     ap.add_argument("--budget", type=int, default=6, help="blocks kept per sequence and head (0: all)")
-    a = ap.parse_args()
+    a = ap.parse_args(argv)
+    if a.tokens < 0:
+        ap.error(f"--tokens {a.tokens}: need 0 or more")
     wl = W.WORKLOADS["tiny"]
     k, n16, n8 = wl.counts()
     lens = [int(x) for x in a.prompt.split(",")]
@@ -187,7 +191,7 @@ def main():
     g.manual_seed(1)
     prompts = [torch.randn((n, wl.d_model), generator=g, device="cuda") for n in lens]
     start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-    run(layers, prompts, 2)  # warm
+    run(layers, prompts, min(a.tokens, 2))  # warm
     for layer in layers:
         layer.cache.reset()
     start.record()
@@ -196,9 +200,10 @@ def main():
     end.synchronize()
     c = layers[0].cache
     used = sum(-(-n // c.block_tokens) for n in held) * c.n_kv_heads * (2 * c.block_tokens * c.head_dim + 8)
+    rms = f", last row's rms {float(rows[-1].square().mean().sqrt()):.3f}" if a.tokens else ""
     print(f"{a.layers} layers of d_model {wl.d_model}: prompts of {lens} tokens, {a.tokens} decoded in "
           f"{start.elapsed_time(end):.1f} ms; the cache holds {held} tokens per sequence "
-          f"({used / 1e6:.2f} MB per layer), last row's rms {float(rows[-1].square().mean().sqrt()):.3f}")
+          f"({used / 1e6:.2f} MB per layer){rms}")
 
 
 if __name__ == "__main__":

@@ -2,6 +2,7 @@
 from types import SimpleNamespace
 
 import pytest
+import torch
 
 from paper_2410_14740_amd import decoder
 
@@ -22,3 +23,14 @@ def test_evict_keeps_within_any_budget(budget):
 def test_a_negative_budget_is_refused():
     with pytest.raises(ValueError, match="budget -1"):
         decoder.DecoderLayer(None, 1, 1, 0, 1, 8, 2, 64, (None, None), budget=-1)
+
+
+def test_a_prompt_without_tokens_is_refused():
+    with pytest.raises(ValueError, match="without tokens"):
+        decoder.run([], [torch.zeros(3, 8), torch.zeros(0, 8)], 1)
+
+
+def test_a_negative_number_of_tokens_is_refused(capsys):
+    with pytest.raises(SystemExit):
+        decoder.main(["--tokens", "-1"])
+    assert "--tokens -1" in capsys.readouterr().err

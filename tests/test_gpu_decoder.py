@@ -130,3 +130,13 @@ def test_decode_with_a_small_budget(budget):
     assert bool(torch.isfinite(rows).all())
     for n, m in zip(held, lens):
         assert (n - 1) // block <= budget and (n - m - steps) % block == 0 and n < m + steps
+
+
+@pytest.mark.parametrize("prompt,tokens", [("64", 0), ("63", 1), ("64,3", 1), ("5", 3)])
+def test_command_of_few_tokens(prompt, tokens, capsys):
+    """Prompts that end at a block's edge, and no or one token after them."""
+    say(f"decoder command {prompt} {tokens}")
+    decoder.main(["--layers", "1", "--prompt", prompt, "--tokens", str(tokens)])
+    held = [int(n) + tokens for n in prompt.split(",")]
+    out = capsys.readouterr().out
+    assert f"{tokens} decoded" in out and f"holds {held}" in out and ("rms" in out) == (tokens > 0)
