@@ -268,6 +268,9 @@ class KVCache:
         dict of tensors "table", "weight", "len" that get the rows instead of
         the cache's own."""
         n, seqs = self._n(seqs, self.n_seqs if seqs is None else seqs.shape[0])
+        for name, v in (("keep", keep), ("first", first), ("recent", recent)):
+            if not 0 <= v < 1 << 31:  # a larger one would be cut to 32 bits on the way
+                _bad(f"{name} {v}: need [0, 2^31 - 1]")
         to = (None, None, None)
         if out is not None:
             to = (out["table"], out["weight"], out["len"])
