@@ -148,11 +148,15 @@ class KVCache:
         if dtype not in _DTYPES:
             _bad(f"dtype {dtype}: need torch.float16 or torch.bfloat16")
         if tensors is not None:
-            dev = tensors["k_codes"].device
-            n_pages = tensors["k_codes"].shape[0]
+            codes = tensors.get("k_codes")
+            if codes is None or not codes.is_cuda or codes.dim() != 3:
+                _bad("tensors: need GPU tensors, k_codes [pages, block_tokens, head_dim] among them")
+            dev, n_pages = codes.device, codes.shape[0]
         else:
             dev = torch.device("cuda", torch.cuda.current_device()) if device is None \
                 else torch.device(device)
+            if dev.type != "cuda":
+                _bad(f"device {dev}: need a GPU")
             if dev.index is None:
                 dev = torch.device("cuda", torch.cuda.current_device())
         entries = n_seqs * n_kv_heads * max_blocks

@@ -20,3 +20,11 @@ def test_evict_refuses_what_32_bits_do_not_hold(args, name):
         c.evict(*args, stream=0)
     assert e.value.status == m2c.M2C_ERR_INVALID_ARG and str(e.value).count(f"{name} ")
     c.evict((1 << 31) - 1, 0, 5, stream=0)
+
+
+def test_a_cache_in_host_memory_is_refused():
+    codes = torch.zeros((4, 64, 64), dtype=torch.int8)
+    for kw in (dict(tensors={"k_codes": codes}), dict(tensors={}), dict(tensors={"k_codes": codes[0]}), dict(device="cpu")):
+        with pytest.raises(m2c.M2CError) as e:
+            attention.KVCache(1, 2, 64, 2, **kw)
+        assert e.value.status == m2c.M2C_ERR_INVALID_ARG
