@@ -25,8 +25,8 @@ __device__ __forceinline__ uint32_t max_mag(uint32_t a, uint32_t b) {
 // exact remainder give that quotient (three operations instead of a division's
 // dozen, which would take longer than the memory); the tests compare every pair
 // of fp16 and of bf16 significands. Adding 1.5 2^23 rounds it to an integer, ties
-// to even, in the low byte. |x| <= 127 s (1 + 2^-23), so nothing has to be
-// clamped.
+// to even, in the low byte. |x| <= 127 s (1 + 2^-23) for a normal s, so nothing
+// has to be clamped.
 template <bool BF>
 __device__ __forceinline__ u32x2 codes_of(u32x4 x, float s, float r) {
   uint32_t t[8];
@@ -45,7 +45,8 @@ __device__ __forceinline__ u32x2 codes_of(u32x4 x, float s, float r) {
 }
 
 // The same by a division, for scales whose reciprocal is not a normal number
-// (bf16 blocks below 2^-93 or above 2^107).
+// (bf16 blocks below 2^-93 or above 2^107). A subnormal s is 2^-133 / 127, 516 of
+// the smallest fp32 number, or more, so |x| <= 127 s (1 + 2^-10): still 127.
 template <bool BF>
 __device__ __forceinline__ u32x2 codes_divided(u32x4 x, float s) {
   u32x2 c = {0, 0};
