@@ -589,6 +589,7 @@ m2c_status m2c_kv_reset(const m2c_kv_cache* cache, const int32_t* seqs, int32_t 
  *             of a block or lie in the last block (M2C_ERR_STATE otherwise)
  *   k_stride, v_stride  token and head strides in elements
  * The weight of every block that gets its first token is set to 0. A sequence
+ * that gets no rows stays as it is, wherever its pos lies. A sequence
  * that would pass max_blocks * block_tokens tokens is M2C_ERR_CAPACITY. */
 m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
                          const int32_t* cu, int64_t total, const int32_t* pos, const void* k,

@@ -24,14 +24,14 @@
 // the same stretch of code as this tile's softmax, which runs beside them. Few
 // rows of many keys are cut along the keys (see Plan).
 //
-// Measured: 64 / 8 heads of 128, bf16, causal, 8192 + 2500 tokens 1110 us, 1.08
-// PFLOP/s (a bf16 product of 8192^3 by the library: 1.25); 32 heads, fp16, seven
-// prompts of 1 .. 2380 tokens 82 us; 40 heads, chunks of 512, 300 and 77 rows
-// against up to 3584 keys 76 us and a join of 4 that finds nothing to do. What
-// bounds it: the matrix instructions are busy in 59% of the cycles, some vector
-// or matrix instruction in 80%; a workgroup alone on its CU takes 1.4 us per tile
-// of keys, two together 1.9 us for both, so the last two cases, whose longest
-// rows are 38 and 56 tiles, wait for those rows.
+// Measured: 64 / 8 heads of 128, bf16, causal, 8192 + 2500 tokens 1105 to 1230 us
+// by the machine's clock, 0.98 to 1.09 PFLOP/s (a bf16 product of 8192^3 by the
+// library: 1.25); 32 heads, fp16, seven prompts of 1 .. 2380 tokens 82 to 88 us; 40
+// heads, chunks of 512, 300 and 77 rows against up to 3584 keys 76 us and a join
+// of 4 that finds nothing to do. What bounds it: the matrix instructions are busy
+// in 59% of the cycles, some vector or matrix instruction in 80%; a workgroup alone
+// on its CU takes 1.4 us per tile of keys, two together 1.9 us for both, so the last
+// two cases, whose longest rows are 38 and 56 tiles, wait for those rows.
 #include <algorithm>
 #include <type_traits>
 

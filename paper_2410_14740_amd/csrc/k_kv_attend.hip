@@ -15,7 +15,8 @@
 // that order. Codes become fp16 exactly; queries of bf16 caches are scaled by a
 // power of two per head into fp16's range (exact but for elements 2^-24 of the
 // head's largest). So both products sum exact products in fp32, p alone is
-// rounded (fp16, relative 2^-12).
+// rounded (relative 2^-11 in fp16; 2^-8 over the open block of a bf16 cache, whose
+// values are bf16).
 //
 // The units of all rows (a row: a sequence, key/value head and tile of 16 query
 // heads), one after another, are cut into even shares, one per workgroup of a
@@ -677,9 +678,9 @@ Split split_of(const KvView& C, int n, int n_heads, int max_len) {
   // length that the caller allows. So there are at most kRounds rounds of
   // them, and the rows' number of parts is odd, so that the first parts, all that
   // short rows have, fall on every XCD (us and MB of workspace with chunks of 16 and
-  // so, 64 / 8 heads: 96 ragged sequences of up to 16000 tokens 407, 51 and 311, 35;
-  // one of 100000 among 127 short ones 246, 417 and 180, 38; 128 of up to 2000 where
-  // 131072 are allowed 256, 550 and 82, 38; 1100 of up to 2100 622, 110 and 437, 0).
+  // so, 64 / 8 heads: 96 ragged sequences of up to 16000 tokens 406, 51 and 314, 35;
+  // one of 100000 among 127 short ones 247, 417 and 181, 38; 128 of up to 2000 where
+  // 131072 are allowed 256, 550 and 79, 38; 1100 of up to 2100 624, 110 and 450, 0).
   constexpr int kRounds = 16;
   int64_t chunk = whole ? units : share > 32 ? std::max<int64_t>(16, (share + kRounds - 1) / kRounds) : share;
   chunk = (chunk + kWaves - 1) / kWaves * kWaves;
