@@ -486,7 +486,8 @@ m2c_status m2c_ratio_search(m2c_layer* layer, const uint16_t* x, int32_t T, int3
  * rounded to the 16-bit type of the matrix instruction that takes them. A
  * masked key contributes nothing, whatever its key and value hold. A query
  * without any key has a zero output and the log-sum-exp -infinity. */
-enum { M2C_DTYPE_FP16 = 0, M2C_DTYPE_BF16 = 1 };
+enum { M2C_DTYPE_FP16 = 0, M2C_DTYPE_BF16 = 1,
+       M2C_DTYPE_FP32 = 2 /* m2c_residual_norm only */ };
 
 typedef struct {
   int32_t dtype;         /* M2C_DTYPE_* of q, k, v and out                      */
@@ -645,6 +646,46 @@ m2c_status m2c_kv_evict(const m2c_kv_cache* cache, const int32_t* seqs, int32_t 
  * the device since the last check: M2C_ERR_INVALID_ARG (a sequence or page out
  * of range, row starts that do not ascend), M2C_ERR_CAPACITY, M2C_ERR_STATE, or M2C_OK. */
 m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Between a layer's blocks: the residual stream and its norms
+ * ------------------------------------------------------------------------
+ * Per row of d elements, x the residual stream, y a block's output:
+ *     t   = N(y) post_weight + post_bias if post, y otherwise
+ *     r   = x + scale gate t                                    (x_out)
+ *     out = N(r) weight + bias                                  (the next block's input)
+ *     N(z) = (z - mean z) / sqrt(mean (z - mean z)^2 + eps), mean z taken as 0
+ *            for M2C_NORM_RMS
+ * All of it in fp32 (sums that leave its range in 64 bits), each output rounded
+ * once: out is of r, not of what x_out's type keeps of it. */
+enum { M2C_NORM_RMS = 0, M2C_NORM_LAYER = 1 };
+
+typedef struct {
+  int32_t kind;          /* M2C_NORM_*, of both norms                           */
+  int32_t post;          /* 1: y is normed before it is added                   */
+  int32_t d;             /* elements of a row, 1..65536                         */
+  int32_t device;        /* HIP device ordinal of every pointer                 */
+  int32_t x_dtype;       /* of x and x_out: M2C_DTYPE_FP32, or the one 16-bit   */
+  int32_t y_dtype;       /* type that the call uses; so are the others          */
+  int32_t out_dtype;
+  int32_t weight_dtype;  /* of weights, biases and gate                         */
+  float eps;             /* >= 0 and finite                                     */
+  float scale;           /* finite                                              */
+  int64_t x_stride, y_stride, x_out_stride, out_stride; /* elements between rows,
+                            0 .. 2^40; rows that are written must not overlap   */
+  int64_t gate_stride;   /* between the rows of gate; 0: one for all            */
+  const void *weight, *bias;           /* dev [d], or NULL: 1 and 0             */
+  const void *post_weight, *post_bias; /* the same; NULL unless post            */
+  const void* gate;      /* dev, or NULL: 1                                     */
+} m2c_norm_desc;
+
+/* One pass over `rows` rows (up to 2^30). y NULL: r = x (no post, gate). x_out
+ * may be x, with its strides, or NULL; out may be NULL; otherwise what is written
+ * must not overlap what is read. Any alignment of whole elements; rows of 16-byte
+ * aligned starts whose length divides by 8 are faster. Results are the same bits
+ * on every run. Only enqueues; keeps no state. */
+m2c_status m2c_residual_norm(const m2c_norm_desc* desc, const void* x, const void* y, int64_t rows,
+                             void* x_out, void* out, void* stream);
 
 /* Test support. Copies one record of the host store (no device work). */
 m2c_status m2c_debug_read_record(const m2c_layer* layer, int32_t tier, int32_t neuron, void* out,

@@ -1,5 +1,6 @@
-// Host side of the attention calls of the C ABI: argument checks and launches.
+// Host side of the attention half's calls of the C ABI: argument checks and launches.
 #include "kv_device.h"
+#include "rows_device.h"
 
 namespace m2c {
 int64_t prompt_workspace(const m2c_attn_desc* D, bool self, int n_seqs, int64_t total_q, int64_t total_k);
@@ -130,6 +131,66 @@ m2c_status check_prompt(const m2c_attn_desc* D, int n_seqs, int64_t total_q, int
   if (total_q < 0 || total_q > kMaxRows || total_k < 0 || total_k > kMaxRows)
     return api_fail(M2C_ERR_INVALID_ARG, "total_q %lld, total_k %lld: need [0, 2^30]",
                     (long long)total_q, (long long)total_k);
+  return M2C_OK;
+}
+
+constexpr int64_t kMaxRowStride = (int64_t)1 << 40;
+
+m2c_status check_norm(const m2c_norm_desc* D, const void* x, const void* y, int64_t rows, const void* x_out,
+                      const void* out) {
+  if (!D) return api_fail(M2C_ERR_INVALID_ARG, "residual norm: NULL argument");
+  if (D->kind != M2C_NORM_RMS && D->kind != M2C_NORM_LAYER)
+    return api_fail(M2C_ERR_INVALID_ARG, "kind %d: need M2C_NORM_RMS or M2C_NORM_LAYER", D->kind);
+  if (D->post != 0 && D->post != 1) return api_fail(M2C_ERR_INVALID_ARG, "post %d: need 0 or 1", D->post);
+  if (D->d < 1 || D->d > 65536) return api_fail(M2C_ERR_INVALID_ARG, "d %d: need [1, 65536]", D->d);
+  if (D->device < 0) return api_fail(M2C_ERR_INVALID_ARG, "device %d", D->device);
+  if (!(D->eps >= 0.0f) || D->eps > 1e30f)
+    return api_fail(M2C_ERR_INVALID_ARG, "eps %g: need >= 0 and finite", (double)D->eps);
+  if (!(D->scale >= -1e30f && D->scale <= 1e30f))
+    return api_fail(M2C_ERR_INVALID_ARG, "scale %g: need a finite number", (double)D->scale);
+  if (rows < 0 || rows > kMaxRows)
+    return api_fail(M2C_ERR_INVALID_ARG, "rows %lld: need [0, 2^30]", (long long)rows);
+  if (rows == 0) return M2C_OK;  // arrays without rows may be NULL
+  if (!x) return api_fail(M2C_ERR_INVALID_ARG, "x: NULL argument");
+  if (!x_out && !out) return api_fail(M2C_ERR_INVALID_ARG, "x_out and out are NULL: nothing to do");
+  if (!y && (D->post || D->gate)) return api_fail(M2C_ERR_INVALID_ARG, "post and gate are y's, and y is NULL");
+  if (!D->post && (D->post_weight || D->post_bias))
+    return api_fail(M2C_ERR_INVALID_ARG, "post_weight, post_bias: need post");
+  const struct {
+    const char* what;
+    const void* p;
+    int dtype;
+    int64_t stride;
+    bool written, rows;
+  } all[] = {{"x", x, D->x_dtype, D->x_stride, false, true},
+             {"y", y, D->y_dtype, D->y_stride, false, true},
+             {"x_out", x_out, D->x_dtype, D->x_out_stride, true, true},
+             {"out", out, D->out_dtype, D->out_stride, true, true},
+             {"gate", D->gate, D->weight_dtype, D->gate_stride, false, true},
+             {"weight", D->weight, D->weight_dtype, 0, false, false},
+             {"bias", D->bias, D->weight_dtype, 0, false, false},
+             {"post_weight", D->post_weight, D->weight_dtype, 0, false, false},
+             {"post_bias", D->post_bias, D->weight_dtype, 0, false, false}};
+  int half = -1;  // the call's 16-bit type
+  for (const auto& a : all) {
+    if (!a.p) continue;
+    if (a.dtype < M2C_DTYPE_FP16 || a.dtype > M2C_DTYPE_FP32)
+      return api_fail(M2C_ERR_INVALID_ARG, "%s: dtype %d: need M2C_DTYPE_*", a.what, a.dtype);
+    if (a.dtype != M2C_DTYPE_FP32) {
+      if (half >= 0 && half != a.dtype)
+        return api_fail(M2C_ERR_INVALID_ARG, "%s: dtype %d: a call has one 16-bit type, here %d", a.what, a.dtype, half);
+      half = a.dtype;
+    }
+    if ((uintptr_t)a.p % (a.dtype == M2C_DTYPE_FP32 ? 4 : 2))
+      return api_fail(M2C_ERR_INVALID_ARG, "%s: not aligned to its elements", a.what);
+    if (!a.rows) continue;
+    if (a.stride < 0 || a.stride > kMaxRowStride)
+      return api_fail(M2C_ERR_INVALID_ARG, "%s: stride %lld: need [0, 2^40]", a.what, (long long)a.stride);
+    if (a.written && rows > 1 && a.stride < D->d)
+      return api_fail(M2C_ERR_INVALID_ARG, "%s: stride %lld: rows overlap", a.what, (long long)a.stride);
+  }
+  if (x_out && x_out == x && rows > 1 && D->x_out_stride != D->x_stride)
+    return api_fail(M2C_ERR_INVALID_ARG, "x_out is x with other strides");
   return M2C_OK;
 }
 
@@ -305,6 +366,15 @@ m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream) {
     return api_fail(M2C_ERR_STATE, "an append's pos was neither the start of a block nor in the last "
                     "block; the sequence was left as it was (status 0x%x)", bits);
   return M2C_OK;
+}
+
+m2c_status m2c_residual_norm(const m2c_norm_desc* D, const void* x, const void* y, int64_t rows, void* x_out,
+                             void* out, void* stream) {
+  CHECKED(check_norm(D, x, y, rows, x_out, out));
+  if (rows == 0) return M2C_OK;
+  CurrentDevice g(D->device);
+  if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", D->device);
+  return launched(m2c::launch_residual_norm(D, x, y, rows, x_out, out, (hipStream_t)stream), "residual norm");
 }
 
 }  // extern "C"

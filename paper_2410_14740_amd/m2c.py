@@ -84,7 +84,8 @@ class DramStats(ctypes.Structure):
                 ("wait_seconds", ctypes.c_double), ("direct_io", ctypes.c_int32)]
 
 
-DTYPE_FP16, DTYPE_BF16 = range(2)
+DTYPE_FP16, DTYPE_BF16, DTYPE_FP32 = range(3)
+NORM_RMS, NORM_LAYER = range(2)
 _I64x2 = ctypes.c_int64 * 2
 
 
@@ -102,6 +103,14 @@ class KvCacheDesc(ctypes.Structure):
         "reserved")] + [("n_pages", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in (
             "k_codes", "v_codes", "k_scale", "v_scale", "tail_k", "tail_v", "table", "len",
             "weight", "arrive", "status")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "kind", "post", "d", "device", "x_dtype", "y_dtype", "out_dtype", "weight_dtype")] + [
+        ("eps", ctypes.c_float), ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "x_stride", "y_stride", "x_out_stride", "out_stride", "gate_stride")] + [
+        (n, ctypes.c_void_p) for n in ("weight", "bias", "post_weight", "post_bias", "gate")]
 
 
 class Stats(ctypes.Structure):
@@ -173,6 +182,7 @@ def load(path: str = LIB_PATH):
                                 P, _I64x2, P, I32, I32, P, I64, P]),
         "m2c_kv_evict": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, I32, I32, P, P, P, P]),
         "m2c_kv_status": (I32, [ctypes.POINTER(KvCacheDesc), P]),
+        "m2c_residual_norm": (I32, [ctypes.POINTER(NormDesc), P, P, I64, P, P, P]),
         "m2c_last_error": (ctypes.c_char_p, []),
         "m2c_build_id": (ctypes.c_char_p, []),
     }
@@ -474,6 +484,10 @@ def m2c_kv_evict(cache: KvCacheDesc, seqs, n: int, keep: int, first: int, recent
 
 def m2c_kv_status(cache: KvCacheDesc, stream=None):
     _check(load().m2c_kv_status(cache, _stream(stream)))
+
+
+def m2c_residual_norm(desc: NormDesc, x, y, rows: int, x_out, out, stream=None):
+    _check(load().m2c_residual_norm(desc, _ptr(x), _ptr(y), rows, _ptr(x_out), _ptr(out), _stream(stream)))
 
 
 def m2c_last_error() -> str:
