@@ -530,6 +530,37 @@ m2c_status m2c_prompt_attention(const m2c_attn_desc* desc, const void* q, const 
                                 int32_t n_seqs, int64_t total_q, int64_t total_k, void* out,
                                 float* lse, void* stream);
 
+/* Rotation of queries and keys by their positions. A pair (a, b) of a head's
+ * first rot_dim elements becomes
+ *     scale (a cos w - b sin w),  scale (b cos w + a sin w),
+ *     w = position * freq[pair],
+ * the other elements stay as they are. A position has n_axes coordinates (time,
+ * height and width, for example); the first section[0] pairs turn by the first,
+ * the next section[1] by the second, and so on. The angle is exact to 2^-51 of
+ * itself, so that far positions turn as near ones do. */
+typedef struct {
+  int32_t rot_dim;       /* a multiple of 16, 16 .. head_dim                    */
+  int32_t interleaved;   /* 1: pair i is elements 2i, 2i + 1; 0: elements i,
+                            i + rot_dim / 2                                     */
+  int32_t n_axes;        /* 1..4                                                */
+  int32_t section[4];    /* pairs of each axis, >= 0 (those past n_axes 0); all
+                            together rot_dim / 2                                */
+  float scale;           /* finite; 0 = 1                                       */
+  const float* freq;     /* dev [rot_dim / 2], radians per position             */
+} m2c_rotary;
+
+/* Rows of queries and keys turned: q_out gets q's [total] rows, k_out k's.
+ *   positions  dev int32, row i's coordinate a at positions[a * pos_stride + i]
+ *   q, k       with their strides (tokens, heads); k NULL: queries alone (n_kv_heads 0)
+ *   q_out may be q with its strides, and k_out k; otherwise what is written must
+ *   not overlap what is read. head_dim 64 or 128. */
+m2c_status m2c_rotate(const m2c_rotary* rotary, int32_t dtype, int32_t head_dim, int32_t device,
+                      int64_t total, const int32_t* positions, int64_t pos_stride, int32_t n_heads,
+                      const void* q, const int64_t q_stride[2], void* q_out,
+                      const int64_t q_out_stride[2], int32_t n_kv_heads, const void* k,
+                      const int64_t k_stride[2], void* k_out, const int64_t k_out_stride[2],
+                      void* stream);
+
 /* Key/value cache. The tokens of a sequence are cut into blocks of
  * block_tokens. A block of one key/value head lies in a page:
  *     amax = max |x| over the block (its keys, and apart its values),
@@ -596,6 +627,26 @@ m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
                          const int32_t* cu, int64_t total, const int32_t* pos, const void* k,
                          const void* v, const int64_t k_stride[2], const int64_t v_stride[2],
                          void* stream);
+
+/* m2c_kv_append with keys that are turned by their positions on the way, rounded
+ * once to the cache's 16-bit type: what the cache holds is to the bit what
+ * m2c_rotate and m2c_kv_append would leave. In the same launch:
+ *   q, q_out   dev [total] rows of n_heads heads, the queries of the same tokens,
+ *              turned as well (q_out may be q with its strides), or NULL
+ *              (n_heads 0)
+ *   k_out      dev [total] rows that get the turned keys too, not k, or NULL
+ * positions and pos_stride are m2c_rotate's; pos is the place in the cache, as in
+ * m2c_kv_append. Queries of every row of a sequence are turned, whatever becomes
+ * of its append; keys of a sequence whose append is refused are not written to
+ * k_out. Rows of no sequence are not written. */
+m2c_status m2c_kv_append_rotated(const m2c_kv_cache* cache, const m2c_rotary* rotary,
+                                 const int32_t* seqs, int32_t n, const int32_t* cu, int64_t total,
+                                 const int32_t* pos, const int32_t* positions, int64_t pos_stride,
+                                 const void* k, const void* v, const int64_t k_stride[2],
+                                 const int64_t v_stride[2], void* k_out,
+                                 const int64_t k_out_stride[2], int32_t n_heads, const void* q,
+                                 const int64_t q_stride[2], void* q_out,
+                                 const int64_t q_out_stride[2], void* stream);
 
 /* Read tokens back in the cache's 16-bit type (code * s rounded once; tokens
  * of the open block as they came): rows cu[b] .. cu[b + 1] - 1 of k and v get

@@ -133,6 +133,75 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, max_q=0, causal=True, scale=None,
     return (out, lse) if return_lse else out
 
 
+class Rotary:
+    """How positions turn the pairs of a head's first 2 len(freq) elements.
+
+    freq: fp32 GPU tensor [pairs], a multiple of 8, radians per position of each
+    pair. sections: pairs of each axis of a position, in order (default: one axis).
+    interleaved: pair i is elements 2i and 2i + 1, not i and i + pairs. scale:
+    a factor of the turned elements."""
+
+    def __init__(self, freq, sections=None, interleaved=False, scale=1.0):
+        if freq.dim() != 1 or freq.dtype != torch.float32 or not freq.is_cuda or not freq.is_contiguous():
+            _bad("freq: need a contiguous fp32 GPU tensor [pairs]")
+        pairs = freq.shape[0]
+        sections = [pairs] if sections is None else list(sections)
+        if pairs % 8 or not 8 <= pairs <= 64:
+            _bad(f"freq: {pairs} pairs, need a multiple of 8, 8 to 64")
+        if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != pairs:
+            _bad(f"sections {sections}: need 1 to 4 counts of pairs, {pairs} in all")
+        if not 0.0 < abs(scale) <= 1e30:
+            _bad(f"scale {scale}: need a finite number other than 0")
+        self.freq, self.axes = freq, len(sections)
+        self.desc = m2c.RotaryDesc(2 * pairs, 1 if interleaved else 0, len(sections),
+                                   (m2c.ctypes.c_int32 * 4)(*sections), scale, freq.data_ptr())
+
+    def _positions(self, positions, rows, device):
+        """Address and axis stride of checked positions."""
+        want = (rows,) if self.axes == 1 and positions.dim() == 1 else (self.axes, rows)
+        if positions.shape != want or positions.dtype != torch.int32 or positions.device != device or \
+                self.freq.device != device or (rows > 1 and positions.stride(-1) != 1):
+            _bad(f"positions: {positions.dtype} {tuple(positions.shape)} on {positions.device}, need int32 "
+                 f"{want} on {device}, as freq is, the coordinates of an axis contiguous")
+        return positions.data_ptr(), (positions.stride(0) if self.axes > 1 else rows)
+
+    def rotate(self, q, positions, k=None, q_out=None, k_out=None, stream=None):
+        """q [tokens, n_heads, head_dim], and k [tokens, n_kv_heads, head_dim] if
+        given, turned by positions (int32 [axes, tokens], or [tokens] for one axis).
+        q_out, k_out: what gets them (may be q and k; allocated if not given).
+        Returns q_out, or (q_out, k_out) where k is given."""
+        if q.dim() != 3 or q.dtype not in _DTYPES or not q.is_cuda:
+            _bad("q: need an fp16 or bf16 GPU tensor [tokens, heads, head_dim]")
+        dev, (n, hq, d) = q.device, q.shape
+        at, step = self._positions(positions, n, dev)
+        q_out, qs, qos = _turned("q", q, q_out, n, hq, d, q.dtype, dev, stream)
+        hk, ks, kos = 0, _NONE, _NONE
+        if k is not None:
+            hk = k.shape[1] if k.dim() == 3 else 0
+            k_out, ks, kos = _turned("k", k, k_out, n, hk, d, q.dtype, dev, stream)
+        elif k_out is not None:
+            _bad("k_out: there is no k")
+        _check(m2c.load().m2c_rotate(self.desc, _DTYPES[q.dtype], d, dev.index, n, at, step, hq, q.data_ptr(), qs,
+                                     q_out.data_ptr(), qos, hk, _address(k), ks, _address(k_out), kos,
+                                     _raw(stream, dev)))
+        return q_out if k is None else (q_out, k_out)
+
+
+_NONE = _I64x2(0, 0)
+
+
+def _turned(name, t, out, tokens, heads, dim, dtype, device, stream):
+    """Where rows go, and the strides of both."""
+    strides = _rows(name, t, dtype, device, heads, dim)
+    if t.shape[0] != tokens:
+        _bad(f"{name}: {t.shape[0]} tokens, need {tokens}")
+    if out is None:
+        return _like(t, stream), strides, _I64x2(heads * dim, dim)
+    if out.shape != t.shape:
+        _bad(f"{name}_out: shape {tuple(out.shape)}, need {tuple(t.shape)}")
+    return out, strides, _rows(name + "_out", out, dtype, device, heads, dim)
+
+
 class KVCache:
     """Keys and values of `n_seqs` sequences in 8 bits, one fp32 scale per
     block of `block_tokens` tokens of a key/value head.
@@ -215,6 +284,39 @@ class KVCache:
         _check(self._lib.m2c_kv_append(self.desc, _address(seqs), n, _address(cu), k.shape[0],
                                        _address(pos), k.data_ptr(), v.data_ptr(), ks, vs,
                                        _raw(stream, self.device)))
+
+    def append_rotated(self, rotary, k, v, positions, q=None, cu=None, seqs=None, pos=None, q_out=None, k_out=None,
+                       stream=None):
+        """`append` of keys that `rotary` turns by `positions` (as in Rotary.rotate;
+        pos is the place in the cache) on the way, and of the queries q [tokens,
+        n_heads, head_dim] of the same tokens beside them. q_out: what gets the
+        queries (may be q; allocated if not given). k_out: rows that get the turned
+        keys as well (not k), True to allocate them. Returns (q_out, k_out), None for
+        what there is not."""
+        n = k.shape[0] if cu is None else cu.shape[0] - 1
+        n, seqs = self._n(seqs, n)
+        dev, hk, d = self.device, self.n_kv_heads, self.head_dim
+        _ints("cu", cu, n + 1, dev)
+        _ints("pos", pos, n, dev)
+        ks = _rows("k", k, self.dtype, dev, hk, d)
+        vs = _rows("v", v, self.dtype, dev, hk, d)
+        rows = k.shape[0]
+        if v.shape[0] != rows:
+            _bad(f"v: {v.shape[0]} tokens, k has {rows}")
+        at, step = rotary._positions(positions, rows, dev)
+        hq, qs, qos, kos = 0, _NONE, _NONE, _NONE
+        if q is not None:
+            hq = q.shape[1] if q.dim() == 3 else 0
+            q_out, qs, qos = _turned("q", q, q_out, rows, hq, d, self.dtype, dev, stream)
+        elif q_out is not None:
+            _bad("q_out: there is no q")
+        if k_out is not None:
+            k_out, _, kos = _turned("k", k, None if k_out is True else k_out, rows, hk, d, self.dtype, dev, stream)
+        _check(self._lib.m2c_kv_append_rotated(
+            self.desc, rotary.desc, _address(seqs), n, _address(cu), rows, _address(pos), at, step, k.data_ptr(),
+            v.data_ptr(), ks, vs, _address(k_out), kos, hq, _address(q), qs, _address(q_out), qos,
+            _raw(stream, dev)))
+        return q_out, k_out
 
     def read(self, cu, total=None, seqs=None, k=None, v=None, stream=None):
         """Tokens 0, 1, .. of sequence seqs[b] into rows cu[b] .. cu[b + 1] - 1

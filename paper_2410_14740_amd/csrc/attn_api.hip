@@ -134,6 +134,46 @@ m2c_status check_prompt(const m2c_attn_desc* D, int n_seqs, int64_t total_q, int
   return M2C_OK;
 }
 
+m2c_status check_rotary(const m2c_rotary* R, int head_dim, const int32_t* positions, int64_t pos_stride,
+                        int64_t total) {
+  if (!R) return api_fail(M2C_ERR_INVALID_ARG, "rotary is NULL");
+  if (R->rot_dim < 16 || R->rot_dim > head_dim || R->rot_dim % 16)
+    return api_fail(M2C_ERR_INVALID_ARG, "rot_dim %d: need a multiple of 16, at most head_dim %d", R->rot_dim, head_dim);
+  if (R->interleaved != 0 && R->interleaved != 1)
+    return api_fail(M2C_ERR_INVALID_ARG, "interleaved %d: need 0 or 1", R->interleaved);
+  if (R->n_axes < 1 || R->n_axes > 4) return api_fail(M2C_ERR_INVALID_ARG, "n_axes %d: need [1, 4]", R->n_axes);
+  int64_t pairs = 0;
+  for (int a = 0; a < 4; ++a) {
+    if (R->section[a] < 0 || (a >= R->n_axes && R->section[a]))
+      return api_fail(M2C_ERR_INVALID_ARG, "section[%d] %d: need >= 0, and 0 past n_axes", a, R->section[a]);
+    pairs += R->section[a];
+  }
+  if (pairs != R->rot_dim / 2)
+    return api_fail(M2C_ERR_INVALID_ARG, "section: %lld pairs, need rot_dim / 2 = %d", (long long)pairs, R->rot_dim / 2);
+  if (!(R->scale >= -1e30f && R->scale <= 1e30f))
+    return api_fail(M2C_ERR_INVALID_ARG, "scale %g: need a finite number", (double)R->scale);
+  if (!R->freq || !positions) return api_fail(M2C_ERR_INVALID_ARG, "freq, positions: NULL argument");
+  if (R->n_axes > 1 && (pos_stride < total || pos_stride > kMaxRows))
+    return api_fail(M2C_ERR_INVALID_ARG, "pos_stride %lld: need [total, 2^30]", (long long)pos_stride);
+  return M2C_OK;
+}
+
+// Rows that are turned into other rows, or in place.
+m2c_status check_turned(const char* what, const char* out_what, const void* p, const int64_t* stride,
+                        const void* out, const int64_t* out_stride, int64_t total, int heads, int head_dim) {
+  if (heads < 1 || heads > 1024) return api_fail(M2C_ERR_INVALID_ARG, "%s: %d heads: need [1, 1024]", what, heads);
+  m2c_status rc = check_rows(what, p, stride, head_dim);
+  if (rc == M2C_OK) rc = check_written(out_what, out, out_stride, total, heads, head_dim);
+  if (rc != M2C_OK) return rc;
+  if (p == out && ((total > 1 && stride[0] != out_stride[0]) || (heads > 1 && stride[1] != out_stride[1])))
+    return api_fail(M2C_ERR_INVALID_ARG, "%s is %s with other strides", out_what, what);
+  return M2C_OK;
+}
+
+m2c::TurnRows turned_rows(const void* p, const int64_t* stride, void* out, const int64_t* out_stride, int heads) {
+  return {(const uint8_t*)p, (uint8_t*)out, stride[0] * 2, stride[1] * 2, out_stride[0] * 2, out_stride[1] * 2, heads};
+}
+
 constexpr int64_t kMaxRowStride = (int64_t)1 << 40;
 
 m2c_status check_norm(const m2c_norm_desc* D, const void* x, const void* y, int64_t rows, const void* x_out,
@@ -263,6 +303,67 @@ m2c_status m2c_kv_append(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_append(C, seqs, n, cu, total, pos, k, v, k_stride, v_stride,
                                         (hipStream_t)stream), "append");
+}
+
+m2c_status m2c_kv_append_rotated(const m2c_kv_cache* cache, const m2c_rotary* rotary, const int32_t* seqs,
+                                 int32_t n, const int32_t* cu, int64_t total, const int32_t* pos,
+                                 const int32_t* positions, int64_t pos_stride, const void* k, const void* v,
+                                 const int64_t k_stride[2], const int64_t v_stride[2], void* k_out,
+                                 const int64_t k_out_stride[2], int32_t n_heads, const void* q,
+                                 const int64_t q_stride[2], void* q_out, const int64_t q_out_stride[2],
+                                 void* stream) {
+  KvView C;
+  CHECKED(view_of(cache, &C));
+  CHECKED(check_n(C, n));
+  if (total < 0 || total > kMaxRows || (!cu && total != n))
+    return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30], and n without cu", (long long)total);
+  if (total == 0) return M2C_OK;
+  CHECKED(check_rotary(rotary, C.head_dim, positions, pos_stride, total));
+  CHECKED(check_rows("k", k, k_stride, C.head_dim));
+  CHECKED(check_rows("v", v, v_stride, C.head_dim));
+  if (k_out) {
+    CHECKED(check_written("k_out", k_out, k_out_stride, total, C.n_kv_heads, C.head_dim));
+    if (k_out == k) return api_fail(M2C_ERR_INVALID_ARG, "k_out is k: keys are read more than once");
+  }
+  m2c::TurnRows Q = {};
+  if (q) {
+    CHECKED(check_turned("q", "q_out", q, q_stride, q_out, q_out_stride, total, n_heads, C.head_dim));
+    Q = turned_rows(q, q_stride, q_out, q_out_stride, n_heads);
+  } else if (n_heads || q_out) {
+    return api_fail(M2C_ERR_INVALID_ARG, "q is NULL, n_heads %d and q_out are not", n_heads);
+  }
+  CurrentDevice g(cache->device);
+  if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
+  return launched(m2c::launch_kv_append_rotated(C, m2c::turn_view(rotary, positions, pos_stride),
+                                                rotary->interleaved != 0, seqs, n, cu, total, pos, k, v, k_stride,
+                                                v_stride, k_out, k_out_stride, Q, (hipStream_t)stream),
+                  "append rotated");
+}
+
+m2c_status m2c_rotate(const m2c_rotary* rotary, int32_t dtype, int32_t head_dim, int32_t device, int64_t total,
+                      const int32_t* positions, int64_t pos_stride, int32_t n_heads, const void* q,
+                      const int64_t q_stride[2], void* q_out, const int64_t q_out_stride[2], int32_t n_kv_heads,
+                      const void* k, const int64_t k_stride[2], void* k_out, const int64_t k_out_stride[2],
+                      void* stream) {
+  CHECKED(check_heads(dtype, 1, 1, head_dim, 0.0f, device));
+  if (total < 0 || total > kMaxRows)
+    return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30]", (long long)total);
+  if (total == 0) return M2C_OK;
+  CHECKED(check_rotary(rotary, head_dim, positions, pos_stride, total));
+  CHECKED(check_turned("q", "q_out", q, q_stride, q_out, q_out_stride, total, n_heads, head_dim));
+  m2c::TurnRows K = {};
+  if (k) {
+    CHECKED(check_turned("k", "k_out", k, k_stride, k_out, k_out_stride, total, n_kv_heads, head_dim));
+    K = turned_rows(k, k_stride, k_out, k_out_stride, n_kv_heads);
+  } else if (n_kv_heads || k_out) {
+    return api_fail(M2C_ERR_INVALID_ARG, "k is NULL, n_kv_heads %d and k_out are not", n_kv_heads);
+  }
+  CurrentDevice g(device);
+  if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", device);
+  return launched(m2c::launch_rotate(m2c::turn_view(rotary, positions, pos_stride), rotary->interleaved != 0,
+                                     dtype == M2C_DTYPE_BF16, head_dim, total,
+                                     turned_rows(q, q_stride, q_out, q_out_stride, n_heads), K, (hipStream_t)stream),
+                  "rotate");
 }
 
 m2c_status m2c_kv_read(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, const int32_t* cu,

@@ -5,6 +5,8 @@
 // append 73 us and read 65 us, each 377 MB (5.2 and 5.8 TB/s; a 1 GiB copy:
 // 5.1). One token for each of 8 sequences of 32 heads: 5 to 7 us, a chain of
 // dependent loads (length, tail, table) and the arrivals at the length.
+#include <algorithm>
+
 #include "kv_device.h"
 
 namespace m2c {
@@ -98,17 +100,50 @@ __device__ __forceinline__ void set_length(const KvView& C, int s, bool placed, 
   else atomicOr(C.status, placed ? kKvCapacity : kKvState);
 }
 
+// How keys go into the cache: as they are, or turned (PAIRS: a pair's sides are
+// neighbours, not half the turned elements apart).
+struct AsTheyAre {
+  static constexpr bool kTurns = false;
+};
+template <bool PAIRS>
+struct TurnAppend {
+  static constexpr bool kTurns = true, kPairs = PAIRS;
+  TurnView T;
+  TurnRows Q;
+  uint8_t* k_out;
+  int64_t ko_tok, ko_head;  // bytes
+  int64_t blocks;           // workgroups that append; the others turn queries
+  int parts;                // of a group of tokens' heads
+};
+
 // One block of one sequence and key/value head. Thread t holds chunk t % (D/8)
 // of tokens t / (D/8), + 256 / (D/8), ..
-template <bool BF, int D, int BT>
+// Keys that turn by their positions are stored in k_out as well, if there is one,
+// and workgroups past the blocks turn the queries.
+template <bool BF, int D, int BT, class How>
 __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32_t* seqs, int n,
                                                      const int32_t* cu, int64_t total,
                                                      const int32_t* pos, const uint8_t* k,
                                                      const uint8_t* v, int64_t k_tok, int64_t k_head,
-                                                     int64_t v_tok, int64_t v_head) {
+                                                     int64_t v_tok, int64_t v_head,
+                                                     const How R) {
   constexpr int CH = D / 8, TP = 256 / CH;  // chunks of a token, tokens a pass of 256 threads takes
   constexpr int NP = BT / TP;
   __shared__ uint32_t mags[2][4];
+  if constexpr (How::kTurns) {
+    __shared__ __align__(16) float2 cs[kTurnTokens][64];
+    if ((int64_t)blockIdx.x >= R.blocks) {
+      const int i = (int)((int64_t)blockIdx.x - R.blocks), g = i / R.parts, part = i - g * R.parts;
+      // rows of no sequence stay as they are
+      const int64_t lo = cu ? clamp64(cu[0], 0, total) : 0, hi = cu ? clamp64(cu[n], lo, total) : total;
+      const int64_t tok0 = lo + (int64_t)g * kTurnTokens;
+      if (tok0 >= hi) return;
+      TurnRows none = {};
+      turn_rows<BF, D, How::kPairs>(R.T, R.Q, none, tok0, (int)(hi - tok0 < kTurnTokens ? hi - tok0 : kTurnTokens),
+                                           part * R.Q.heads / R.parts, (part + 1) * R.Q.heads / R.parts, cs);
+      return;
+    }
+  }
   const int x = blockIdx.x / C.n_kv_heads, head = blockIdx.x - x * C.n_kv_heads, tid = threadIdx.x;
   int b = x, item = 0, items = 1;
   int64_t row0 = b;
@@ -140,6 +175,17 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
     const uint8_t* kr = k + row0 * k_tok + head * k_head;
     const uint8_t* vr = v + row0 * v_tok + head * v_head;
     const int ch = tid % CH, t0 = tid / CH;
+    // 16 bytes of a new token's key
+    auto new_key = [&](int64_t r) {
+      if constexpr (How::kTurns)
+        return turn_chunk<BF, How::kPairs>(R.T, kr + r * k_tok, row0 + r, ch);
+      else
+        return *(const u32x4*)(kr + r * k_tok + ch * 16);
+    };
+    auto keep_key = [&](int64_t r, u32x4 x) {
+      if constexpr (How::kTurns)
+        if (R.k_out) *(u32x4*)(R.k_out + (row0 + r) * R.ko_tok + head * R.ko_head + ch * 16) = x;
+    };
     // Item 0 takes the first block, which may begin in the tail, and then
     // writes the tail of the last block; the others never touch the tail.
     for (int blk = first + item; blk <= last; blk += items) {
@@ -154,7 +200,14 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
         const int t = t0 + i * TP;
         const bool old = at + t < p0;
         const int64_t r = at + t - p0;
-        xk[i] = *(const u32x4*)((old ? tk + t * (D * 2) : kr + r * k_tok) + ch * 16);
+        if constexpr (!How::kTurns) {
+          xk[i] = *(const u32x4*)((old ? tk + t * (D * 2) : kr + r * k_tok) + ch * 16);
+        } else if (old) {
+          xk[i] = *(const u32x4*)(tk + t * (D * 2) + ch * 16);
+        } else {
+          xk[i] = new_key(r);
+          keep_key(r, xk[i]);
+        }
         xv[i] = *(const u32x4*)((old ? tv + t * (D * 2) : vr + r * v_tok) + ch * 16);
       }
 #pragma unroll
@@ -196,7 +249,9 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
       for (int t = t0; t < BT; t += TP) {
         if (at + t < p0 || at + t >= end) continue;
         const int64_t r = at + t - p0;
-        *(u32x4*)(tk + t * (D * 2) + ch * 16) = *(const u32x4*)(kr + r * k_tok + ch * 16);
+        const u32x4 key = new_key(r);
+        if (at + BT > end) keep_key(r, key);  // those of a full block are stored already
+        *(u32x4*)(tk + t * (D * 2) + ch * 16) = key;
         *(u32x4*)(tv + t * (D * 2) + ch * 16) = *(const u32x4*)(vr + r * v_tok + ch * 16);
       }
     }
@@ -325,21 +380,52 @@ hipError_t by_shape(const KvView& C, F f) {
 
 }  // namespace
 
-hipError_t launch_kv_append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,
-                            int64_t total, const int32_t* pos, const void* k, const void* v,
-                            const int64_t* ks, const int64_t* vs, hipStream_t stream) {
+namespace {
+
+template <class How>
+hipError_t append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu, int64_t total,
+                  const int32_t* pos, const void* k, const void* v, const int64_t* ks, const int64_t* vs,
+                  How R, hipStream_t stream) {
   const int64_t items = cu ? total / C.block_tokens + 2 * (int64_t)n : n;
-  if (items * C.n_kv_heads > INT32_MAX) return hipErrorInvalidValue;
+  int64_t grid = items * C.n_kv_heads;
+  if constexpr (How::kTurns) {
+    R.blocks = grid;
+    const int64_t groups = (total + kTurnTokens - 1) / kTurnTokens;
+    R.parts = (int)std::min<int64_t>(std::max<int64_t>(512 / groups, 1), (R.Q.heads + 7) / 8);
+    grid += groups * R.parts;
+  }
+  if (grid > INT32_MAX) return hipErrorInvalidValue;
   const hipError_t e = by_shape(C, [&](auto bf, auto d, auto bt) {
-    hipLaunchKernelGGL((append_kernel<decltype(bf)::value, decltype(d)::value, decltype(bt)::value>),
-                       dim3((uint32_t)(items * C.n_kv_heads)), dim3(256), 0, stream, C, seqs, n, cu,
+    hipLaunchKernelGGL((append_kernel<decltype(bf)::value, decltype(d)::value, decltype(bt)::value, How>),
+                       dim3((uint32_t)grid), dim3(256), 0, stream, C, seqs, n, cu,
                        total, pos, (const uint8_t*)k, (const uint8_t*)v, ks[0] * 2, ks[1] * 2,
-                       vs[0] * 2, vs[1] * 2);
+                       vs[0] * 2, vs[1] * 2, R);
     return hipGetLastError();
   });
   if (e != hipSuccess || !cu) return e;
   hipLaunchKernelGGL(length_kernel, dim3((n + 255) / 256), dim3(256), 0, stream, C, seqs, n, cu, total, pos);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,
+                            int64_t total, const int32_t* pos, const void* k, const void* v,
+                            const int64_t* ks, const int64_t* vs, hipStream_t stream) {
+  return append(C, seqs, n, cu, total, pos, k, v, ks, vs, AsTheyAre(), stream);
+}
+
+hipError_t launch_kv_append_rotated(const KvView& C, const TurnView& T, bool interleaved, const int32_t* seqs,
+                                    int n, const int32_t* cu, int64_t total, const int32_t* pos, const void* k,
+                                    const void* v, const int64_t* ks, const int64_t* vs, void* k_out,
+                                    const int64_t* kos, const TurnRows& Q, hipStream_t stream) {
+  const auto go = [&](auto how) {
+    how.T = T, how.Q = Q;
+    how.k_out = (uint8_t*)k_out;
+    how.ko_tok = k_out ? kos[0] * 2 : 0, how.ko_head = k_out ? kos[1] * 2 : 0;
+    return append(C, seqs, n, cu, total, pos, k, v, ks, vs, how, stream);
+  };
+  return interleaved ? go(TurnAppend<true>()) : go(TurnAppend<false>());
 }
 
 hipError_t launch_kv_read(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,

@@ -3,7 +3,7 @@
 
 #include <type_traits>
 
-#include "attn_device.h"
+#include "rotary_device.h"
 
 namespace m2c {
 
@@ -26,6 +26,10 @@ struct KvView {
 hipError_t launch_kv_append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,
                             int64_t total, const int32_t* pos, const void* k, const void* v,
                             const int64_t* ks, const int64_t* vs, hipStream_t stream);
+hipError_t launch_kv_append_rotated(const KvView& C, const TurnView& T, bool interleaved, const int32_t* seqs,
+                                    int n, const int32_t* cu, int64_t total, const int32_t* pos, const void* k,
+                                    const void* v, const int64_t* ks, const int64_t* vs, void* k_out,
+                                    const int64_t* kos, const TurnRows& Q, hipStream_t stream);
 hipError_t launch_kv_read(const KvView& C, const int32_t* seqs, int n, const int32_t* cu,
                           int64_t total, void* k, void* v, const int64_t* ks, const int64_t* vs,
                           hipStream_t stream);

@@ -105,6 +105,11 @@ class KvCacheDesc(ctypes.Structure):
             "weight", "arrive", "status")]
 
 
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "n_axes")] + [
+        ("section", ctypes.c_int32 * 4), ("scale", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+
 class NormDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "kind", "post", "d", "device", "x_dtype", "y_dtype", "out_dtype", "weight_dtype")] + [
@@ -176,6 +181,11 @@ def load(path: str = LIB_PATH):
         "m2c_kv_reset": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P]),
         "m2c_kv_append": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, P, P, P, _I64x2, _I64x2,
                                 P]),
+        "m2c_kv_append_rotated": (I32, [ctypes.POINTER(KvCacheDesc), ctypes.POINTER(RotaryDesc), P, I32, P, I64,
+                                        P, P, I64, P, P, _I64x2, _I64x2, P, _I64x2, I32, P, _I64x2, P, _I64x2,
+                                        P]),
+        "m2c_rotate": (I32, [ctypes.POINTER(RotaryDesc), I32, I32, I32, I64, P, I64, I32, P, _I64x2, P, _I64x2,
+                             I32, P, _I64x2, P, _I64x2, P]),
         "m2c_kv_read": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, P, P, _I64x2, _I64x2, P]),
         "m2c_kv_attend_workspace": (I64, [ctypes.POINTER(KvCacheDesc), I32, I32, I32, I32]),
         "m2c_kv_attend": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, ctypes.c_float, P, _I64x2,
@@ -453,6 +463,23 @@ def m2c_kv_append(cache: KvCacheDesc, seqs, n: int, cu, total: int, pos, k, v, k
                   stream=None):
     _check(load().m2c_kv_append(cache, _ptr(seqs), n, _ptr(cu), total, _ptr(pos), _ptr(k), _ptr(v),
                                 _I64x2(*k_stride), _I64x2(*v_stride), _stream(stream)))
+
+
+def m2c_kv_append_rotated(cache: KvCacheDesc, rotary: RotaryDesc, seqs, n: int, cu, total: int, pos, positions,
+                          pos_stride: int, k, v, k_stride, v_stride, k_out=None, k_out_stride=(0, 0),
+                          n_heads: int = 0, q=None, q_stride=(0, 0), q_out=None, q_out_stride=(0, 0), stream=None):
+    _check(load().m2c_kv_append_rotated(cache, rotary, _ptr(seqs), n, _ptr(cu), total, _ptr(pos), _ptr(positions),
+                                        pos_stride, _ptr(k), _ptr(v), _I64x2(*k_stride), _I64x2(*v_stride),
+                                        _ptr(k_out), _I64x2(*k_out_stride), n_heads, _ptr(q), _I64x2(*q_stride),
+                                        _ptr(q_out), _I64x2(*q_out_stride), _stream(stream)))
+
+
+def m2c_rotate(rotary: RotaryDesc, dtype: int, head_dim: int, device: int, total: int, positions, pos_stride: int,
+               n_heads: int, q, q_stride, q_out, q_out_stride, n_kv_heads: int = 0, k=None, k_stride=(0, 0),
+               k_out=None, k_out_stride=(0, 0), stream=None):
+    _check(load().m2c_rotate(rotary, dtype, head_dim, device, total, _ptr(positions), pos_stride, n_heads, _ptr(q),
+                             _I64x2(*q_stride), _ptr(q_out), _I64x2(*q_out_stride), n_kv_heads, _ptr(k),
+                             _I64x2(*k_stride), _ptr(k_out), _I64x2(*k_out_stride), _stream(stream)))
 
 
 def m2c_kv_read(cache: KvCacheDesc, seqs, n: int, cu, total: int, k, v, k_stride, v_stride,
