@@ -677,6 +677,41 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
                          void* out, const int64_t out_stride[2], float* lse, int32_t track,
                          int32_t max_len, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* Bytes of the workspace with which m2c_kv_attend_chunk with the same arguments
+ * splits the queries that see many more keys than the others along them (0 where
+ * it would split none), or -1. */
+int64_t m2c_kv_attend_chunk_workspace(const m2c_kv_cache* cache, int32_t n, int64_t total,
+                                      int32_t n_heads, int32_t max_q, int32_t max_len);
+
+/* Attention of chunks of tokens: rows cu[b] .. cu[b + 1] - 1 of q and out are
+ * sequence seqs[b]'s (which may be listed twice). Its keys are the tokens that the
+ * cache holds and then, where k and v are given, the same rows of k and v: the
+ * chunk's own, which are not in the cache yet (append them afterwards). With k and
+ * v NULL the cache holds the chunk already. Of nk keys in all, query i of lq sees
+ * keys 0 .. nk - lq + i. The cache is not changed.
+ *   cu         dev int32 [n + 1], ascending, within [0, total]; rows of no sequence
+ *              are not written
+ *   q, out     dev [total] rows of n_heads heads, with their strides
+ *   k, v       dev [total] rows of the cache's heads, with their strides, or both NULL
+ *   scale      factor of <q, k>; 0 = 1 / sqrt(head_dim)
+ *   lse        dev fp32 [total][n_heads] or NULL
+ *   max_q, max_len  longest chunk, and most tokens that a sequence of the call
+ *              holds in the cache, or 0 if not known: only help to choose whether
+ *              rows are split along their keys
+ *   workspace  dev, 256-byte aligned, not shared with a call that may run at the
+ *              same time, or NULL: no row is split
+ * A sequence id out of range is reported, its rows become zeros (lse -infinity);
+ * row starts that do not ascend are reported and touch nothing out of range.
+ * bf16 caches: blocks of values whose scale is below 2^-80 of another's, or of the
+ * 16-bit values', may count as larger, up to that. Results are the same bits on every run with the same arguments. */
+m2c_status m2c_kv_attend_chunk(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
+                               const int32_t* cu, int64_t total, int32_t n_heads, float scale,
+                               const void* q, const int64_t q_stride[2], const void* k,
+                               const int64_t k_stride[2], const void* v, const int64_t v_stride[2],
+                               void* out, const int64_t out_stride[2], float* lse, int32_t max_q,
+                               int32_t max_len, void* workspace, int64_t workspace_bytes,
+                               void* stream);
+
 /* Evict blocks by accumulated weight. The last block of a sequence always
  * stays; of the m blocks before it every key/value head keeps
  * `keep` if m > keep (all of them otherwise): the first `first`, the last

@@ -368,6 +368,50 @@ class KVCache:
                                        max_len, _address(work), need, _raw(stream, self.device)))
         return (out, lse) if return_lse else out
 
+    def attend_chunk(self, q, cu, k=None, v=None, seqs=None, max_q=0, max_len=0, scale=None, out=None,
+                     return_lse=False, stream=None):
+        """Attention of chunks of tokens: rows cu[b] .. cu[b + 1] - 1 of q [tokens,
+        n_heads, head_dim] are sequence seqs[b]'s (default: b). Its keys are what the
+        cache holds of it and then the same rows of k and v [tokens, n_kv_heads,
+        head_dim], the chunk's own, which are appended afterwards; without them the
+        cache holds the chunk already. Of nk keys in all, query i of lq sees keys 0
+        .. nk - lq + i. max_q, max_len: longest chunk, and most tokens of a sequence
+        in the cache, if known. scale: as in prompt_attention.
+        Returns out like q, or (out, lse) with lse fp32 [tokens, n_heads]."""
+        if q.dim() != 3 or cu.dim() != 1:
+            _bad("q: need [tokens, n_heads, head_dim]; cu: row starts and the end")
+        total, hq, dev = q.shape[0], q.shape[1], self.device
+        n, seqs = self._n(seqs, cu.shape[0] - 1)
+        _ints("cu", cu, n + 1, dev)
+        qs = _rows("q", q, self.dtype, dev, hq, self.head_dim)
+        if (k is None) != (v is None):
+            _bad("attend_chunk: give k and v, or neither")
+        ks = vs = _NONE
+        if k is not None:
+            ks = _rows("k", k, self.dtype, dev, self.n_kv_heads, self.head_dim)
+            vs = _rows("v", v, self.dtype, dev, self.n_kv_heads, self.head_dim)
+            if k.shape[0] != total or v.shape[0] != total:
+                _bad(f"k, v: {k.shape[0]} and {v.shape[0]} tokens, q has {total}")
+        key = (n, total, hq, max_q, max_len)
+        need = self._need.get(key)
+        if need is None:
+            if len(self._need) >= 4096:
+                self._need.clear()
+            need = self._need[key] = m2c.m2c_kv_attend_chunk_workspace(self.desc, *key)
+        if out is None:
+            out, os = _like(q, stream), _I64x2(hq * self.head_dim, self.head_dim)
+        elif out.shape != q.shape:
+            _bad(f"out: shape {tuple(out.shape)}, need {tuple(q.shape)}")
+        else:
+            os = _rows("out", out, self.dtype, dev, hq, self.head_dim)
+        lse = _alloc(stream, dev, ((total, hq), torch.float32))[0] if return_lse else None
+        work = _alloc(stream, dev, ((need,), torch.uint8))[0] if need else None
+        _check(self._lib.m2c_kv_attend_chunk(
+            self.desc, _address(seqs), n, cu.data_ptr(), total, hq, 0.0 if scale is None else scale, q.data_ptr(), qs,
+            _address(k), ks, _address(v), vs, out.data_ptr(), os, _address(lse), max_q, max_len, _address(work), need,
+            _raw(stream, dev)))
+        return (out, lse) if return_lse else out
+
     def evict(self, keep, first=0, recent=0, seqs=None, out=None, stream=None):
         """Keep `keep` blocks before the last one of every listed sequence and
         head: the first `first`, the last `recent`, else the heaviest. out: a

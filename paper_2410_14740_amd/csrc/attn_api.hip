@@ -119,6 +119,19 @@ m2c_status check_n(const KvView& C, int n) {
   return M2C_OK;
 }
 
+m2c_status check_chunk(const m2c_kv_cache* cache, const KvView& C, int n, int64_t total, int n_heads, float scale,
+                       int max_q, int max_len) {
+  // a sequence may be listed more than once
+  if (n < 1 || n > 65535) return api_fail(M2C_ERR_INVALID_ARG, "n %d: need [1, 65535]", n);
+  const m2c_status rc = check_heads(cache->dtype, n_heads, C.n_kv_heads, C.head_dim, scale, cache->device);
+  if (rc != M2C_OK) return rc;
+  if (total < 0 || total > kMaxRows)
+    return api_fail(M2C_ERR_INVALID_ARG, "total %lld: need [0, 2^30]", (long long)total);
+  if (max_q < 0 || max_len < 0)
+    return api_fail(M2C_ERR_INVALID_ARG, "max_q %d, max_len %d: need >= 0", max_q, max_len);
+  return M2C_OK;
+}
+
 m2c_status check_prompt(const m2c_attn_desc* D, int n_seqs, int64_t total_q, int64_t total_k) {
   if (!D) return api_fail(M2C_ERR_INVALID_ARG, "prompt attention: NULL argument");
   const m2c_status rc = check_heads(D->dtype, D->n_heads, D->n_kv_heads, D->head_dim, D->scale, D->device);
@@ -419,6 +432,46 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
   if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
   return launched(m2c::launch_kv_attend(C, seqs, n, n_heads, scale, q, q_stride, out, out_stride, lse,
                                         track, max_len, workspace, (hipStream_t)stream), "attend");
+}
+
+int64_t m2c_kv_attend_chunk_workspace(const m2c_kv_cache* cache, int32_t n, int64_t total, int32_t n_heads,
+                                      int32_t max_q, int32_t max_len) {
+  KvView C;
+  if (view_of(cache, &C) != M2C_OK || check_chunk(cache, C, n, total, n_heads, 0.0f, max_q, max_len) != M2C_OK)
+    return -1;
+  return total ? m2c::kv_chunk_workspace(C, n, n_heads, total, max_q, max_len) : 0;
+}
+
+m2c_status m2c_kv_attend_chunk(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, const int32_t* cu,
+                               int64_t total, int32_t n_heads, float scale, const void* q,
+                               const int64_t q_stride[2], const void* k, const int64_t k_stride[2],
+                               const void* v, const int64_t v_stride[2], void* out,
+                               const int64_t out_stride[2], float* lse, int32_t max_q, int32_t max_len,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+  KvView C;
+  CHECKED(view_of(cache, &C));
+  CHECKED(check_chunk(cache, C, n, total, n_heads, scale, max_q, max_len));
+  if (!cu) return api_fail(M2C_ERR_INVALID_ARG, "cu is NULL");
+  if (total == 0) return M2C_OK;
+  CHECKED(check_rows("q", q, q_stride, C.head_dim));
+  CHECKED(check_written("out", out, out_stride, total, n_heads, C.head_dim));
+  if (!k != !v) return api_fail(M2C_ERR_INVALID_ARG, "k, v: both or none");
+  if (k) {
+    CHECKED(check_rows("k", k, k_stride, C.head_dim));
+    CHECKED(check_rows("v", v, v_stride, C.head_dim));
+  }
+  if (workspace) {
+    const int64_t need = m2c::kv_chunk_workspace(C, n, n_heads, total, max_q, max_len);
+    if ((uintptr_t)workspace & 255) return api_fail(M2C_ERR_INVALID_ARG, "workspace: not 256-byte aligned");
+    if (workspace_bytes < need)
+      return api_fail(M2C_ERR_CAPACITY, "workspace of %lld bytes: need %lld", (long long)workspace_bytes,
+                      (long long)need);
+  }
+  CurrentDevice g(cache->device);
+  if (!g.ok) return api_fail(M2C_ERR_INVALID_ARG, "device %d is not usable", cache->device);
+  return launched(m2c::launch_kv_chunk(C, seqs, n, cu, total, n_heads, scale, q, q_stride, k, k_stride, v, v_stride,
+                                       out, out_stride, lse, max_q, max_len, workspace, (hipStream_t)stream),
+                  "attend chunk");
 }
 
 m2c_status m2c_kv_evict(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n, int32_t keep,

@@ -38,6 +38,11 @@ int64_t kv_attend_workspace(const KvView& C, int n, int n_heads, int track, int 
 hipError_t launch_kv_attend(const KvView& C, const int32_t* seqs, int n, int n_heads, float scale,
                             const void* q, const int64_t* qs, void* out, const int64_t* os,
                             float* lse, int track, int max_len, void* workspace, hipStream_t stream);
+int64_t kv_chunk_workspace(const KvView& C, int n, int n_heads, int64_t total, int max_q, int max_len);
+hipError_t launch_kv_chunk(const KvView& C, const int32_t* seqs, int n, const int32_t* cu, int64_t total,
+                           int n_heads, float scale, const void* q, const int64_t* qs, const void* k,
+                           const int64_t* ks, const void* v, const int64_t* vs, void* out, const int64_t* os,
+                           float* lse, int max_q, int max_len, void* workspace, hipStream_t stream);
 hipError_t launch_kv_evict(const KvView& C, const int32_t* seqs, int n, int keep, int first,
                            int recent, int32_t* table_out, float* weight_out, int32_t* len_out,
                            hipStream_t stream);

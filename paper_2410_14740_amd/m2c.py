@@ -190,6 +190,9 @@ def load(path: str = LIB_PATH):
         "m2c_kv_attend_workspace": (I64, [ctypes.POINTER(KvCacheDesc), I32, I32, I32, I32]),
         "m2c_kv_attend": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, ctypes.c_float, P, _I64x2,
                                 P, _I64x2, P, I32, I32, P, I64, P]),
+        "m2c_kv_attend_chunk_workspace": (I64, [ctypes.POINTER(KvCacheDesc), I32, I64, I32, I32, I32]),
+        "m2c_kv_attend_chunk": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, P, I64, I32, ctypes.c_float, P, _I64x2, P,
+                                      _I64x2, P, _I64x2, P, _I64x2, P, I32, I32, P, I64, P]),
         "m2c_kv_evict": (I32, [ctypes.POINTER(KvCacheDesc), P, I32, I32, I32, I32, P, P, P, P]),
         "m2c_kv_status": (I32, [ctypes.POINTER(KvCacheDesc), P]),
         "m2c_residual_norm": (I32, [ctypes.POINTER(NormDesc), P, P, I64, P, P, P]),
@@ -501,6 +504,22 @@ def m2c_kv_attend(cache: KvCacheDesc, seqs, n: int, n_heads: int, scale: float, 
     _check(load().m2c_kv_attend(cache, _ptr(seqs), n, n_heads, scale, _ptr(q), _I64x2(*q_stride),
                                 _ptr(out), _I64x2(*out_stride), _ptr(lse), track, max_len,
                                 _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def m2c_kv_attend_chunk_workspace(cache: KvCacheDesc, n: int, total: int, n_heads: int, max_q: int, max_len: int) -> int:
+    need = load().m2c_kv_attend_chunk_workspace(cache, n, total, n_heads, max_q, max_len)
+    if need < 0:
+        raise M2CError(M2C_ERR_INVALID_ARG, load().m2c_last_error().decode())
+    return need
+
+
+def m2c_kv_attend_chunk(cache: KvCacheDesc, seqs, n: int, cu, total: int, n_heads: int, scale: float, q, q_stride,
+                        k, k_stride, v, v_stride, out, out_stride, lse=None, max_q: int = 0, max_len: int = 0,
+                        workspace=None, workspace_bytes: int = 0, stream=None):
+    _check(load().m2c_kv_attend_chunk(cache, _ptr(seqs), n, _ptr(cu), total, n_heads, scale, _ptr(q),
+                                      _I64x2(*q_stride), _ptr(k), _I64x2(*k_stride), _ptr(v), _I64x2(*v_stride),
+                                      _ptr(out), _I64x2(*out_stride), _ptr(lse), max_q, max_len, _ptr(workspace),
+                                      workspace_bytes, _stream(stream)))
 
 
 def m2c_kv_evict(cache: KvCacheDesc, seqs, n: int, keep: int, first: int, recent: int,
