@@ -77,6 +77,15 @@ __device__ __forceinline__ void load_lds16(u32x4 buf, uint32_t off, uint32_t dst
       : "memory");
 }
 
+// The kernel's arguments by a pointer that the compiler cannot tell from others:
+// what is read by it is read again, not kept in registers.
+template <class Args>
+__device__ __forceinline__ const Args* args_again() {
+  uint64_t p = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return (const Args*)(const __attribute__((address_space(4))) Args*)(uintptr_t)p;
+}
+
 // LDS reads by byte address.
 template <typename T>
 __device__ __forceinline__ const __attribute__((address_space(3))) T* lds_at(uint32_t addr) {

@@ -112,13 +112,6 @@ __device__ __forceinline__ void wave_rows_plain(const PromptArgs& A, const uint8
   }
 }
 
-// The kernel's arguments by a pointer that the compiler cannot tell from others.
-__device__ __forceinline__ const PromptArgs* args_again() {
-  uint64_t p = (uint64_t)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(p));
-  return (const PromptArgs*)(const __attribute__((address_space(4))) PromptArgs*)(uintptr_t)p;
-}
-
 template <bool BF, int D, bool SPLIT>
 __global__ void __launch_bounds__(kWaves * 64, 2) prompt_attention_kernel(const PromptArgs A) {
   constexpr int NW = kWaves;
@@ -367,7 +360,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) prompt_attention_kernel(const 
       for (int i = 0; i < 2; ++i) s0[i] = s1[i];
     }
   }
-  const PromptArgs& B = *args_again();
+  const PromptArgs& B = *args_again<PromptArgs>();
   const int64_t first = clamp64(B.cu_q[b], 0, B.total_q);
   uint8_t* ob = B.out + first * B.o_tok + head * B.o_head;
   float* lse = B.lse ? B.lse + first * B.n_heads + head : nullptr;

@@ -47,14 +47,20 @@ struct ChunkArgs : RowArgs {
 
 namespace {
 
-constexpr int kUnitF16 = -24;  // u of fp16 caches: their scales are 2^-31 and more, or 0
+// Values lie in LDS as in the attention of prompts, and a bit further apart: where a
+// wave writes two rows at once, one's 16-byte chunks are even and the other's odd.
+template <int D>
+__device__ __forceinline__ int swz_values(int row) {
+  return D == 128 ? (row & 3) << 2 | (row & 1) : ((row >> 1) & 1) * 5;
+}
 
-// What a wave knows of 64 blocks, lane i of the i-th: its page (-1: none, taken as
-// zeros), key scale, g and 2^-g.
-struct Blocks {
-  int page;
-  float ks, g, inv;
+// A block's key scale and the logarithm of its value scale, -1000 for a scale of 0;
+// NaN for scales that are not finite.
+struct Block {
+  float ks, g;
 };
+
+constexpr int kUnitF16 = -24;  // u of fp16 caches: their scales are 2^-31 and more, or 0
 
 template <bool BF, int D, bool SPLIT>
 __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const ChunkArgs A) {
@@ -68,6 +74,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
   constexpr int KS = D / 16, DT = D / 32;
   __shared__ __align__(1024) uint8_t lds[2][2][kTileBytes];
   __shared__ float weights[NW][16][32];  // of 16 keys, where a value is not finite
+  __shared__ Block blocks[2][64];        // of 64 blocks each, the even and the odd 64s
+  __shared__ int pages[2][64];
 
   // What is wrong with the call is reported once.
   if (blockIdx.x == 0)
@@ -144,7 +152,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
   const uint32_t k_lane = lds_base + col * kRowBytes + ((h ^ swz_k<D>(col)) * 16);
   const int vr = 4 * h + ((lane & 15) >> 2);
   const uint32_t v_lane = lds_base + kTileBytes + vr * kRowBytes +
-                          (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swz_v<D>(vr)) * 16) + (lane & 1) * 8;
+                          (((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ swz_values<D>(vr)) * 16) + (lane & 1) * 8;
 
   f32x16 o[DT];
 #pragma unroll
@@ -153,9 +161,13 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
     for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
-  // S^T of the tile in slot t & 1, on T's instructions.
-  auto scores = [&](int t, f32x16 (&s)[2], auto bf_t) {
-    const uint32_t ka = k_lane + (t & 1) * (2 * kTileBytes);
+  // The tile in slot t & 1. f, g, inv: of its two halves; left: the keys of it that
+  // the lane's row sees (used if MASKED).
+  auto compute = [&](int t, const float (&f)[2], const float (&g)[2], const float (&inv)[2], int left,
+                     auto codes_t, auto masked_t) {
+    constexpr bool CODES = decltype(codes_t)::value, MASKED = decltype(masked_t)::value, B16 = BF && !CODES;
+    const uint32_t ka = k_lane + (t & 1) * (2 * kTileBytes), va = v_lane + (t & 1) * (2 * kTileBytes);
+    f32x16 s[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -164,17 +176,9 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
     for (int ks = 0; ks < KS; ++ks) {
       const u32x4 k_0 = *lds_at<u32x4>(ka ^ (ks * 32));
       const u32x4 k_1 = *lds_at<u32x4>((ka ^ (ks * 32)) + 32 * kRowBytes);
-      s[0] = mfma32<decltype(bf_t)::value>(k_0, qf[ks], s[0]);
-      s[1] = mfma32<decltype(bf_t)::value>(k_1, qf[ks], s[1]);
+      s[0] = mfma32<B16>(k_0, qf[ks], s[0]);
+      s[1] = mfma32<B16>(k_1, qf[ks], s[1]);
     }
-  };
-  // The tile in slot t & 1 from its scores s, and the scores of the next one into
-  // sn. f, g, inv: of its two halves of 32 keys; left: the keys of it that the
-  // lane's row sees (used if MASKED).
-  auto compute = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2], const float (&f)[2], const float (&g)[2],
-                     const float (&inv)[2], int left, auto codes_t, auto masked_t) {
-    constexpr bool CODES = decltype(codes_t)::value, MASKED = decltype(masked_t)::value, B16 = BF && !CODES;
-    const uint32_t va = v_lane + (t & 1) * (2 * kTileBytes);
     if constexpr (MASKED) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -201,7 +205,6 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
     }
-    scores(t + 1, sn, std::integral_constant<bool, B16>());
     const float base = (m == -INFINITY ? 0.0f : m) - kLift;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const u32x2 w = *lds_at<u32x2>(vt + key * kRowBytes + (((dt * 4 + i) ^ swz_v<D>(key)) * 16) + h * 8);
+                const u32x2 w = *lds_at<u32x2>(vt + key * kRowBytes + (((dt * 4 + i) ^ swz_values<D>(key)) * 16) + h * 8);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   const float v = unpack16<BF>(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
@@ -281,7 +284,6 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
     asm volatile("" ::: "memory");
   };
 
-  f32x16 s0[2], s1[2];
   // The 16-bit keys: tiles of the open block, then of the chunk's own.
   {
     const int t0 = max(ta, page_tiles), nt = tb - t0;
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
       const uint8_t* at = open ? (values ? tv : tk) + (int64_t)(k0 - K.paged) * kRowBytes
                                : (values ? A.v + new_v : A.k + new_k) + (k0 - K.held) * step;
       const u32x4 buf = buffer_of(at, (uint32_t)(left * step) + kRowBytes);  // rows past the end are zeros
-      const int swz = values ? swz_v<D>(ld_row) : swz_k<D>(ld_row);
+      const int swz = values ? swz_values<D>(ld_row) : swz_k<D>(ld_row);
       const uint32_t first = (uint32_t)(ld_row * step) + ((lane % kChunks) ^ swz) * 16;
       const uint32_t row_step = (uint32_t)(NW * kLoadRows * step);
 #pragma unroll
@@ -311,40 +313,37 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
         load_lds16(buf, first + i * row_step,
                    lds0 + (values ? kTileBytes : 0) + (t & 1) * (2 * kTileBytes) + i * (NW * 1024));
     };
-    auto arrive = [&](int t) {
-      // this wave's loads have landed, and its reads of K(t) and V(t - 1) are done
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      barrier();
-      if (t + 2 < nt) load_tile(t + 2, false);
-      if (t + 1 < nt) load_tile(t + 1, true);
-    };
+    const float f[2] = {A.c, A.c}, none[2] = {0.0f, 0.0f};
     if (nt > 0) {
       load_tile(0, false);
       load_tile(0, true);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    }
+    auto arrive = [&](int t) {
+      // this wave's loads have landed, and its reads of the tile before are done
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
       barrier();
-      if (nt > 1) load_tile(1, false);
-      scores(0, s0, std::integral_constant<bool, BF>());
-    }
-    const float f[2] = {A.c, A.c}, none[2] = {0.0f, 0.0f};
-    auto whole = [&](int t) { return r0 < rows && first_of(t) + kTileK <= min(wv_lo, end_of(t)); };
-    for (int t = 0; t < nt;) {
-      if (t + 1 < nt && whole(t) && whole(t + 1)) {
-        arrive(t);
-        compute(t, s0, s1, f, none, none, 0, std::false_type(), std::false_type());
-        arrive(t + 1);
-        compute(t + 1, s1, s0, f, none, none, 0, std::false_type(), std::false_type());
-        t += 2;
-      } else {
-        arrive(t);
-        if (first_of(t) < wv_hi) {
-          compute(t, s0, s1, f, none, none, min(seen, end_of(t)) - first_of(t), std::false_type(), std::true_type());
-#pragma unroll
-          for (int i = 0; i < 2; ++i) s0[i] = s1[i];
-        }
-        ++t;
+      if (t + 1 < nt) {
+        load_tile(t + 1, false);
+        load_tile(t + 1, true);
       }
+    };
+    auto some = [&](int from, int to) {
+      for (int t = from; t < to; ++t) {
+        arrive(t);
+        if (first_of(t) < wv_hi)
+          compute(t, f, none, none, min(seen, end_of(t)) - first_of(t), std::false_type(), std::true_type());
+      }
+    };
+    // tiles of the chunk's own keys that every row of the wave sees whole
+    const int own = max(0, page_tiles + open_tiles - t0), before = max(0, t0 - page_tiles - open_tiles);
+    const int whole = r0 >= rows ? 0 : max(0, (wv_lo - K.held) / kTileK - before);
+    const int from = min(max(nt, 0), own), to = min(max(nt, 0), own + whole);
+    some(0, from);
+    for (int t = from; t < to; ++t) {
+      arrive(t);
+      compute(t, f, none, none, 0, std::false_type(), std::false_type());
     }
+    some(max(from, to), nt);
   }
 
   // The pages.
@@ -374,66 +373,27 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
         }
       qc = ldexpf(A.c, -up);
     }
-    const int32_t* table = A.C.table + sh * A.C.max_blocks;
-    const int n_blocks = K.paged >> shift;
-    // 64 blocks at a time: `next` as soon as a load needs them, `now` when the
-    // products have come to them, fewer tiles later than 64 blocks have
-    Blocks next = {-1, 1.0f, 0.0f, 1.0f}, now = next;
-    int next_at = -1, now_at = -1;
-    bool unit_set = false;
-    int o_top = -1000;  // O's numbers are below 2^o_top
-    if constexpr (BF) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int e = __float_as_uint(o[dt][r]) >> 23 & 0xff;
-          o_top = max(o_top, e < 255 ? e - 126 : -1000);
-        }
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) o_top = max(o_top, __shfl_xor(o_top, d));
-    }
-    auto look_up = [&](int w) {
-      const int i = w * 64 + lane;
-      int page = -1;
-      float ks = 0.0f, vs = 0.0f;
-      if (i < n_blocks) {
-        page = table[i];
-        if (page < 0 || page >= A.C.n_pages) {
-          if (wave == 0) atomicOr(A.C.status, kKvBadIndex);
-          page = -1;
-        } else {
-          ks = A.C.k_scale[page];
-          vs = A.C.v_scale[page];
-        }
-      }
-      const bool some = vs > 0.0f && vs < INFINITY;
-      const int e = some ? __builtin_amdgcn_frexp_expf(vs) : -1000;  // vs is in [2^(e - 1), 2^e)
-      if constexpr (BF) {
-        // The unit: 2^-20 of the first blocks' largest scale, or 2^-100 of what O
-        // has by now, and a larger one should later blocks be 2^40 times as large.
-        int top = e;
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) top = max(top, __shfl_xor(top, d));
-        if (top > (unit_set ? u + 60 : -1000)) {
-          const int up = (unit_set ? top - 20 : max(top - 20, o_top - 100)) - u;
-          u += up;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], -up);
-          if (unit_set) now.g -= (float)up, now.inv = ldexpf(now.inv, up);  // (else it has no values)
-          unit_set = true;
-        }
-      }
-      next.page = page;
-      next.ks = ks == 0.0f ? 1.0f : ks < INFINITY ? ks : NAN;  // all codes are 0: any factor will do
-      // scales below 2^-60 units count as 2^-60
-      next.g = some ? fmaxf(log2_fast(__builtin_amdgcn_frexp_mantf(vs)) + (float)(e - u), -60.0f)
-               : vs == 0.0f ? 0.0f : NAN;
-      next.inv = vs < INFINITY ? exp2_fast(-next.g) : 1.0f;
-      next_at = w;
+    const ChunkArgs& P = *args_again<ChunkArgs>();
+    const int32_t* table = P.C.table + sh * P.C.max_blocks;
+    const int n_blocks = K.paged >> shift, n_pages = (int)P.C.n_pages;
+    // What a block's scales come to is looked up for 64 blocks at a time, by one wave,
+    // a lane each. A page out of range, or none, is -1.
+    auto look_page = [&](int w) {
+      const int blk = w * 64 + lane, page = table[min(blk, n_blocks - 1)];
+      const bool in = page >= 0 && page < n_pages;
+      if (blk < n_blocks && !in) atomicOr(P.C.status, kKvBadIndex);
+      return blk < n_blocks && in ? page : -1;
     };
+    auto look_up = [&](int w, int page, float ks, float vs) {
+      const float g = log2_fast(__builtin_amdgcn_frexp_mantf(vs)) + (float)__builtin_amdgcn_frexp_expf(vs);
+      pages[w & 1][lane] = page;
+      blocks[w & 1][lane] = page < 0 ? Block{0.0f, -1000.0f} : Block{fmaf(ks, 0.0f, ks), vs == 0.0f ? -1000.0f : fmaf(vs, 0.0f, g)};
+    };
+    const int w0 = (ta * kTileK) >> shift >> 6;
+    if (wave < 2) {
+      const int page = look_page(w0 + wave);
+      look_up(w0 + wave, page, P.C.k_scale[max(page, 0)], P.C.v_scale[max(page, 0)]);
+    }
     if constexpr (!BF) {
       u = kUnitF16;
 #pragma unroll
@@ -441,35 +401,50 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], -u);
     }
-
+    // u of bf16 caches: 2^-20 of the first block's scale that is not 0, or 2^-100 of
+    // what O has by then, and a larger one should a later scale be 2^40 times as large.
+    bool unit_set = !BF;
+    auto set_unit = [&](int e) __attribute__((always_inline)) {  // for a scale in [2^(e - 1), 2^e)
+      int up = e - 20 - u;
+      if (!unit_set) {
+        int top = -1000;  // O's numbers are below 2^top
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int x = __float_as_uint(o[dt][r]) >> 23 & 0xff;
+            top = max(top, x < 255 ? x - 126 : -1000);
+          }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) top = max(top, __shfl_xor(top, d));
+        up = max(up, __builtin_amdgcn_readfirstlane(top) - 100);
+        unit_set = true;
+      }
+      u += up;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], -up);
+    };
     // A wave's rows of a tile are 16 wave .. + 15: lane i takes chunk i % kCodeChunks
     // of rows i / kCodeChunks, + 64 / kCodeChunks.
     const int c_row = lane / kCodeChunks, c_chunk = lane % kCodeChunks;
     u32x4 rk[CL], rv[CL];
-    int page = -1, in_page = 0;  // of the last tile of keys that was asked for, this wave's rows
-    auto load_rows = [&](const int8_t* codes, u32x4 (&x)[CL]) {
-      if (page >= 0) {
-        const int8_t* p = codes + (((int64_t)page << shift) + in_page) * D + lane * 16;
+    auto load_codes = [&](int t, int page) {  // a page of -1 loads zeros
+      const int64_t at = (((int64_t)max(page, 0) << shift) + (((ta + t) * kTileK + 16 * wave) & (BT - 1))) * D;
+      const int bytes = page < 0 ? 0 : 16 * D;
+      const auto kr = __builtin_amdgcn_make_buffer_rsrc(P.C.k_codes + at, 0, bytes, 0x00020000);
+      const auto vr = __builtin_amdgcn_make_buffer_rsrc(P.C.v_codes + at, 0, bytes, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < CL; ++i) x[i] = *(const u32x4*)(p + i * 1024);
-      } else {
+      for (int i = 0; i < CL; ++i) rk[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, lane * 16 + i * 1024, 0, 0));
 #pragma unroll
-        for (int i = 0; i < CL; ++i) x[i] = u32x4{0, 0, 0, 0};
-      }
+      for (int i = 0; i < CL; ++i) rv[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, lane * 16 + i * 1024, 0, 0));
     };
-    auto load_k = [&](int t) {
-      const int key = (ta + t) * kTileK + 16 * wave, blk = key >> shift;
-      if (blk >> 6 != next_at) look_up(blk >> 6);
-      page = __builtin_amdgcn_readlane(next.page, blk & 63);
-      in_page = key & (BT - 1);
-      load_rows(A.C.k_codes, rk);
-    };
-    auto load_v = [&] { load_rows(A.C.v_codes, rv); };  // of that tile, before the next one's keys
     auto write_codes = [&](int t, const u32x4 (&x)[CL], bool values) {
 #pragma unroll
       for (int i = 0; i < CL; ++i) {
         const int row = 16 * wave + c_row + i * (64 / kCodeChunks);
-        const int swz = values ? swz_v<D>(row) : swz_k<D>(row);
+        const int swz = values ? swz_values<D>(row) : swz_k<D>(row);
         const uint32_t at = lds_base + (t & 1) * (2 * kTileBytes) + (values ? kTileBytes : 0) + row * kRowBytes;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -482,64 +457,80 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
         }
       }
     };
-    // Before tile t is computed K(t + 1) and V(t) are in LDS and K(t + 2) and V(t + 1)
-    // on their way into registers.
-    auto arrive = [&](int t) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's writes, and its reads of K(t) and V(t - 1)
-      barrier();
-      if (t + 2 < nt) write_codes(t + 2, rk, false);
-      if (t + 1 < nt) write_codes(t + 1, rv, true);
-      if (t + 2 < nt) load_v();
-      if (t + 3 < nt) load_k(t + 3);
+    auto block_of = [&](int t, int key) { return ((ta + t) * kTileK + key) >> shift; };
+    // Tile t is computed while t + 1 goes into LDS and t + 2 comes into registers.
+    int page_of = -1;  // that of the wave's rows of tile t + 3
+    auto ask_page = [&](int t) {
+      const int blk = block_of(t, 16 * wave);
+      page_of = pages[blk >> 6 & 1][blk & 63];
     };
-    float f[2], g[2], inv[2];
-    auto scales = [&](int t) {
-      const int w = (ta + t) * kTileK >> shift >> 6;
-      if (w != now_at) now = next, now_at = w;
+    int next_at = -1, next_page = -1;  // the following 64 blocks: which, their pages and scales
+    float next_ks = 0.0f, next_vs = 0.0f;
+    auto look_ahead = [&](int t) {  // in three steps, so that none has to wait
+      const int blk = block_of(t, 0), w = blk >> 6;
+      if ((w & 3) != wave) return;
+      if ((blk & 63) == 8) {
+        next_page = look_page(next_at = w + 1);
+      } else if (next_at != w + 1) {
+        return;  // begun after the first step: looked up before the first tile
+      } else if ((blk & 63) == 16) {
+        next_ks = P.C.k_scale[max(next_page, 0)], next_vs = P.C.v_scale[max(next_page, 0)];
+      } else if ((blk & 63) == 24) {
+        look_up(w + 1, next_page, next_ks, next_vs);
+      }
+    };
+    auto meet = [&] {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's writes, and its reads of the tile before
+      barrier();
+    };
+    auto turn = [&](int t) {
+      meet();
+      if (t + 1 < nt) {
+        write_codes(t + 1, rk, false);
+        write_codes(t + 1, rv, true);
+      }
+      if (t + 2 < nt) load_codes(t + 2, __builtin_amdgcn_readfirstlane(page_of));
+      ask_page(t + 3);
+    };
+    auto attend = [&](int t, auto masked_t) {
+      Block b[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int at = ((ta + t) * kTileK + 32 * i) >> shift & 63;
-        f[i] = qc * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.ks), at));
-        g[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.g), at));
-        inv[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now.inv), at));
+        const int blk = block_of(t, 32 * i);
+        b[i] = blocks[blk >> 6 & 1][blk & 63];
       }
+      if constexpr (BF) {
+        const float top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(fmaxf(b[0].g, b[1].g))));
+        if (top > (unit_set ? (float)(u + 60) : -999.0f)) set_unit((int)floorf(top) + 1);
+      }
+      float f[2], g[2], inv[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f[i] = qc * b[i].ks;
+        const float e = fmaxf(b[i].g - (float)u, -60.0f);  // scales below 2^-60 units count as 2^-60
+        g[i] = fmaf(b[i].g, 0.0f, e), inv[i] = exp2_fast(-e);
+      }
+      compute(t, f, g, inv, min(seen, K.paged) - (ta + t) * kTileK, std::true_type(), masked_t);
     };
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();  // the tiles before are read
-    load_k(0);
-    now = next, now_at = next_at;
-    load_v();
+    const int plain = r0 >= rows ? 0 : min(nt, min(wv_lo, K.paged) / kTileK - ta);  // tiles that all its rows see whole
+    meet();  // the tiles before are read, and the first blocks looked up
+    ask_page(0);
+    load_codes(0, __builtin_amdgcn_readfirstlane(page_of));
+    ask_page(1);
     write_codes(0, rk, false);
-    if (nt > 1) load_k(1);
     write_codes(0, rv, true);
-    if (nt > 1) {
-      load_v();
-      write_codes(1, rk, false);
-    }
-    if (nt > 2) load_k(2);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    barrier();
-    scores(0, s0, std::false_type());
-    const int see_all = min(wv_lo, K.paged) / kTileK - ta;  // tiles that every row of the wave sees whole
-    const int plain = r0 >= rows ? 0 : min(nt, see_all);
+    if (1 < nt) load_codes(1, __builtin_amdgcn_readfirstlane(page_of));
+    ask_page(2);
     int t = 0;
-    for (; t + 1 < plain; t += 2) {
-      arrive(t);
-      scales(t);
-      compute(t, s0, s1, f, g, inv, 0, std::true_type(), std::false_type());
-      arrive(t + 1);
-      scales(t + 1);
-      compute(t + 1, s1, s0, f, g, inv, 0, std::true_type(), std::false_type());
+    for (; t < plain; ++t) {
+      turn(t);
+      attend(t, std::false_type());
+      look_ahead(t);
     }
     for (; t < nt; ++t) {
-      arrive(t);
-      const int k0 = (ta + t) * kTileK;
-      if (k0 < wv_hi) {
-        scales(t);
-        compute(t, s0, s1, f, g, inv, min(seen, K.paged) - k0, std::true_type(), std::true_type());
-#pragma unroll
-        for (int i = 0; i < 2; ++i) s0[i] = s1[i];
-      }
+      turn(t);
+      if ((ta + t) * kTileK < wv_hi) attend(t, std::true_type());
+      look_ahead(t);
     }
   }
 

@@ -46,6 +46,20 @@ def starts(lens):
     return torch.tensor(np.cumsum([0, *lens]), dtype=torch.int32, device="cuda")
 
 
+_made = []
+
+
+@pytest.fixture(autouse=True)
+def clean():
+    """Poisoned memory does not go back to the allocator, which other tests take
+    memory from without filling it."""
+    yield
+    for c in _made:
+        for t in (c.k_codes, c.v_codes, c.k_scale, c.v_scale, c.tail_k, c.tail_v):
+            t.zero_()
+    _made.clear()
+
+
 def make(n, hk, d, block, dtype, lens, seed=1, sigma=1.0, spare=0):
     """A cache that holds `lens` tokens, its pages in no order, its unused places poisoned."""
     mb = max(-(-max(lens) // block), 1) + spare
@@ -56,6 +70,7 @@ def make(n, hk, d, block, dtype, lens, seed=1, sigma=1.0, spare=0):
     c.k_codes.fill_(77), c.v_codes.fill_(-77)
     c.k_scale.fill_(math.nan), c.v_scale.fill_(math.inf)
     c.tail_k.fill_(math.nan), c.tail_v.fill_(math.inf)
+    _made.append(c)
     if sum(lens):
         c.append(rand((sum(lens), hk, d), dtype, seed + 1, sigma), rand((sum(lens), hk, d), dtype, seed + 2, sigma), cu=starts(lens))
     c.check()
@@ -149,6 +164,9 @@ def test_chunk(hq, hk, d, block, dt, lens, ql, how):
 
 LONG = [  # few rows on many keys: rows are cut along them
     (2, 1, 128, 64, BF16, [5000], [1]), (64, 8, 128, 64, F16, [9000, 300, 2000], [5, 5, 5]), (8, 8, 64, 32, F16, [3000, 40], [70, 900]),
+    # parts that are longer than what is looked up at a time, and begin anywhere in it
+    (32, 32, 64, 64, F16, [30000, 21111, 17000, 26001], [2, 1, 3, 2]), (32, 16, 64, 32, BF16, [24000, 9111, 17007], [3, 2, 1]),
+    (16, 16, 64, 128, BF16, [60000, 41111, 57000, 36001], [2, 1, 3, 2]),
     (4, 2, 128, 128, BF16, [6017, 0], [130, 20]), (1, 1, 128, 32, F16, [12345], [300]), (8, 1, 64, 64, BF16, [20000, 1], [17, 200]),
 ]
 
