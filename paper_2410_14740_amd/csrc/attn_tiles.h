@@ -38,6 +38,7 @@ struct Keys {
 
 // Arguments of the kernels on tiles of rows. Beside these a kernel's have
 //   Keys keys(int b) const     of sequence b of the call
+//   kOneRound                  whether parts of rows grow until all run at once
 struct RowArgs {
   const uint8_t* q;
   uint8_t* out;
@@ -189,6 +190,18 @@ __device__ __forceinline__ Plan plan_of(const Args& A) {
   const bool even = (float)wave_max((uint32_t)kt) <= kUneven * share;
   P.most = even ? 1 << 25 : (int)fminf(fmaxf((float)kLeast, ceilf(share)), 0x1p25f);
   P.most = __builtin_amdgcn_readfirstlane(P.most);
+  if constexpr (Args::kOneRound) {
+    // Somewhat larger parts where shares come to a few more than run at once: those
+    // would run alone afterwards.
+    const int rows = __builtin_amdgcn_readlane(wave_incl_scan((uint32_t)P.rows), 63);
+    const bool grow = rows * A.units <= kShares && !__builtin_amdgcn_readfirstlane(even);
+    for (int i = 0; i < 16 && grow; ++i) {
+      const int per = P.keyed > 0 ? (kt + P.most - 1) / P.most : 1;
+      const int items = per > 1 ? P.keyed * per + P.rows - P.keyed : P.rows;
+      if (__builtin_amdgcn_readlane(wave_incl_scan((uint32_t)items), 63) * A.units <= kShares) break;
+      P.most = __builtin_amdgcn_readfirstlane(P.most + max(1, P.most >> 4));
+    }
+  }
   int cut;
   for (;; P.most *= 2) {  // ends: no sequence has more than 2^24 tiles
     P.per = P.keyed > 0 ? (kt + P.most - 1) / P.most : 1;

@@ -39,6 +39,7 @@
 namespace m2c {
 
 struct PromptArgs : RowArgs {
+  static constexpr bool kOneRound = false;
   const uint8_t *k, *v;
   const int32_t* cu_k;
   int64_t total_k;

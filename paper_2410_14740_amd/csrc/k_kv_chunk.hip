@@ -27,6 +27,7 @@
 namespace m2c {
 
 struct ChunkArgs : RowArgs {
+  static constexpr bool kOneRound = true;
   KvView C;
   const int32_t* seqs;
   const uint8_t *k, *v;  // the chunk's keys and values, or NULL: the cache has them
