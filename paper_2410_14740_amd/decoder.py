@@ -13,10 +13,12 @@ One layer, rows x [tokens][d_model] (the residual stream, fp32):
     x += FFN(norm(x))                       (m2c_predict_rank .. m2c_sparse_ffn)
 
 A prompt goes in chunks: a chunk's queries see the tokens before it as the
-cache gives them back (`KVCache.read`) and their own, unrounded, and the chunk
-is then appended. A token is appended and attended over the cache. Keys are
-rotated before they are cached, so evicting blocks leaves the others' positions
-as they are. Projections, norms and rotations are torch's.
+cache holds them (`KVCache.attend_chunk`) and their own, unrounded, and the chunk
+is then appended. A token is rotated on its way into the cache
+(`KVCache.append_rotated`) and attended over it. Keys are rotated before they are
+cached, so evicting blocks leaves the others' positions as they are. The sum into
+the stream after the attention is one with the norm for the FFN
+(`norms.residual_norm`). Projections are torch's.
 """
 from __future__ import annotations
 
@@ -27,21 +29,14 @@ import torch
 
 from . import m2c
 from . import workloads as W
-from .attention import KVCache, prompt_attention
+from .attention import KVCache, Rotary, prompt_attention
+from .norms import residual_norm
 
 
-def norm(x):
-    """Root-mean-square norm of fp32 rows, as fp16 rows."""
-    return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)).half()
-
-
-def rotate(x, pos):
-    """Rotary position embedding of x [tokens][heads][dim] at positions pos [tokens]."""
-    half = x.shape[-1] // 2
-    freq = 10000.0 ** (-torch.arange(half, device=x.device, dtype=torch.float32) / half)
-    a = pos.float()[:, None, None] * freq
-    lo, hi = x[..., :half].float(), x[..., half:].float()
-    return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1).to(x.dtype)
+def rotary(dim, device="cuda"):
+    """The rotation of a head of `dim` elements whose pairs turn once in 2 pi 10000^(2 i / dim) positions."""
+    half = dim // 2
+    return Rotary(10000.0 ** (-torch.arange(half, device=device, dtype=torch.float32) / half))
 
 
 class DecoderLayer:
@@ -60,18 +55,19 @@ class DecoderLayer:
         self.n_heads, self.n_kv_heads, self.dim = n_heads, n_kv_heads, d // n_heads
         self.wqkv, self.wo = weights  # [d][(n_heads + 2 n_kv_heads) dim], [d][d]
         self.budget = budget
+        self.rotary = rotary(self.dim)
         self.cache = KVCache(n_seqs, n_kv_heads, self.dim, -(-max_tokens // block_tokens), block_tokens)
         self.tiers = torch.empty((ffn.desc.max_batch, ffn.desc.d_ff), dtype=torch.uint8, device="cuda")
 
-    def project(self, x, pos):
+    def project(self, x):
+        """Queries, keys and values of rows of the stream, not rotated yet."""
         h, g = self.n_heads, self.n_kv_heads
-        rows = (norm(x) @ self.wqkv).view(x.shape[0], h + 2 * g, self.dim)
-        qk = rotate(rows[:, :h + g], pos)
-        return qk[:, :h], qk[:, h:], rows[:, h + g:]
+        rows = (residual_norm(x)[1] @ self.wqkv).view(x.shape[0], h + 2 * g, self.dim)
+        return rows[:, :h], rows[:, h:h + g], rows[:, h + g:]
 
-    def feed_forward(self, x):
-        """x += FFN(norm(x)), max_batch rows at a time."""
-        rows = norm(x)
+    def feed_forward(self, x, attended):
+        """x += attended Wo, x += FFN(norm(x)), max_batch rows at a time."""
+        _, rows = residual_norm(x, attended.reshape(x.shape[0], -1) @ self.wo, x_out=x)
         for a in range(0, x.shape[0], self.ffn.desc.max_batch):
             part = rows[a:a + self.ffn.desc.max_batch]
             n, L = part.shape[0], self.ffn
@@ -84,30 +80,25 @@ class DecoderLayer:
     def prefill(self, x, lens, before):
         """A chunk of every sequence: rows x are lens[b] tokens of sequence b,
         whose cache holds before[b]. Host lists; x is updated in place."""
-        pos = torch.cat([torch.arange(p, p + n, device="cuda") for n, p in zip(lens, before)])
-        q, k, v = self.project(x, pos)
+        pos = torch.cat([torch.arange(p, p + n, dtype=torch.int32, device="cuda") for n, p in zip(lens, before)])
+        q, k, v = self.project(x)
         cu = _starts(lens)
         if not any(before):
+            q, k = self.cache.append_rotated(self.rotary, k, v, pos, q=q, cu=cu, k_out=True)
             out = prompt_attention(q, k, v, cu, max_q=max(lens))
         else:
-            both = [n + p for n, p in zip(lens, before)]
-            cu_k = _starts(both)
-            kk, vv = self.cache.read(cu_k, sum(both))
-            at = torch.cat([torch.arange(e - n, e, device="cuda") for n, e in zip(lens, np.cumsum(both).tolist())])
-            kk[at], vv[at] = k, v
-            out = prompt_attention(q, kk, vv, cu, cu_k, max_q=max(lens))
-        self.cache.append(k, v, cu=cu)
-        x += out.reshape(x.shape[0], -1) @ self.wo
-        self.feed_forward(x)
+            self.rotary.rotate(q, pos, k=k, q_out=q, k_out=k)
+            out = self.cache.attend_chunk(q, cu, k, v, max_q=max(lens), max_len=max(before))
+            self.cache.append(k, v, cu=cu)
+        self.feed_forward(x, out)
 
     def decode(self, x, pos, max_len):
         """One token per sequence at positions pos (int32 tensor); max_len: the
         longest sequence afterwards. x is updated in place."""
-        q, k, v = self.project(x, pos)
-        self.cache.append(k, v)
+        q, k, v = self.project(x)
+        q, _ = self.cache.append_rotated(self.rotary, k, v, pos, q=q)
         out = self.cache.attend(q, max_len=max_len, track=self.budget > 0)
-        x += out.reshape(x.shape[0], -1) @ self.wo
-        self.feed_forward(x)
+        self.feed_forward(x, out)
 
     def evict(self, first=1, recent=2):
         """Blocks beyond the budget leave, not the first `first` and the last
