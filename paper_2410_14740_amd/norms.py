@@ -25,10 +25,19 @@ def _matrix(name, t, shape, device):
     return a if shape[0] > 1 else shape[1]
 
 
+def _empty(x, dtype, stream):
+    """Rows like x, contiguous (the usual case by the shorter call)."""
+    if stream is None and x.is_contiguous():
+        return torch.empty_like(x, dtype=dtype)
+    return _alloc(stream, x.device, (x.shape, dtype))[0]
+
+
 def _vector(name, t, d, dtype, device):
-    if t is not None and (t.shape != (d,) or t.dtype != dtype or t.device != device or not t.is_contiguous()):
+    if t is None:
+        return None
+    if (t.shape != (d,) or t.dtype != dtype or t.device != device or not t.is_contiguous()):
         _bad(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, need a contiguous {dtype} ({d},) on {device}")
-    return _address(t)
+    return t.data_ptr()
 
 
 def residual_norm(x, y=None, weight=None, bias=None, *, post=False, post_weight=None, post_bias=None, gate=None,
@@ -49,8 +58,11 @@ def residual_norm(x, y=None, weight=None, bias=None, *, post=False, post_weight=
     if kind not in _KINDS:
         _bad(f"kind {kind!r}: need 'rms' or 'layer'")
     dev, shape, d = x.device, x.shape, x.shape[1]
-    vectors = [t for t in (weight, bias, post_weight, post_bias, gate) if t is not None]
-    wt = vectors[0].dtype if vectors else torch.float32
+    wt = torch.float32
+    for t in (weight, bias, post_weight, post_bias, gate):
+        if t is not None:
+            wt = t.dtype
+            break
     if wt not in _DTYPES:
         _bad(f"weights: {wt}, need fp16, bf16 or fp32")
     xs, ys, gs = _matrix("x", x, shape, dev), 0, 0
@@ -64,7 +76,7 @@ def residual_norm(x, y=None, weight=None, bias=None, *, post=False, post_weight=
         else:
             _vector("gate", gate, d, wt, dev)
     if x_out is None:
-        r = x if y is None else _alloc(stream, dev, (shape, x.dtype))[0]
+        r = x if y is None else _empty(x, x.dtype, stream)
     else:
         r = x_out
         if r.dtype != x.dtype:
@@ -77,10 +89,12 @@ def residual_norm(x, y=None, weight=None, bias=None, *, post=False, post_weight=
             return x, None
     elif out is None:
         if out_dtype is None:
-            out_dtype = next((t.dtype for t in (y, x) if t is not None and t.dtype != torch.float32), torch.float16)
+            out_dtype = y.dtype if y is not None and y.dtype != torch.float32 else x.dtype
+            if out_dtype == torch.float32:
+                out_dtype = torch.float16
         if out_dtype not in _DTYPES:
             _bad(f"out_dtype {out_dtype}: need fp16, bf16 or fp32")
-        out, = _alloc(stream, dev, (shape, out_dtype))
+        out = _empty(x, out_dtype, stream)
     elif out_dtype is not None and out.dtype != out_dtype:
         _bad(f"out: {out.dtype}, out_dtype is {out_dtype}")
     os = _matrix("out", out, shape, dev) if out is not None else 0
