@@ -24,54 +24,53 @@ struct NormArgs {
   int x32, y32, o32, w32;  // which are fp32
 };
 
-// 8 elements of a thread's step; ones past the row's end are zeros. VEC: of an
-// aligned row whose length divides by 8, i the index of the 8; otherwise single
-// elements i, i + step, ..
+// Elements 8 i .. 8 i + 7 of a row; ones past its end are zeros. VEC: the row is
+// aligned to 16 bytes and its length divides by 8. Otherwise the same wide loads,
+// which global memory takes at any element's address, and the last few one by one.
+template <int ALIGN, typename T>
+struct Unaligned {
+  typedef T type __attribute__((aligned(ALIGN)));
+};
+
 template <bool BF, bool VEC>
-__device__ __forceinline__ void load8(const uint8_t* row, bool f32, int i, int step, int d, float (&v)[8]) {
-  if constexpr (VEC) {
-    if (8 * i >= d) {
+__device__ __forceinline__ void load8(const uint8_t* row, bool f32, int i, int d, float (&v)[8]) {
+  const int64_t at = (int64_t)i * 8;
+  if (VEC ? 8 * i >= d : 8 * i + 8 > d) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    } else if (f32) {
-      const f32x4 a = *(const f32x4*)(row + (int64_t)i * 32), b = *(const f32x4*)(row + (int64_t)i * 32 + 16);
+    for (int j = 0; j < 8; ++j)
+      v[j] = VEC || at + j >= d ? 0.0f
+             : f32              ? *(const float*)(row + (at + j) * 4)
+                                : unpack16<BF>(*(const uint16_t*)(row + (at + j) * 2));
+  } else if (f32) {
+    typedef typename Unaligned<VEC ? 16 : 4, f32x4>::type Four;
+    const f32x4 a = *(const Four*)(row + at * 4), b = *(const Four*)(row + at * 4 + 16);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = j < 4 ? a[j % 4] : b[j % 4];
-    } else {
-      const u32x4 a = *(const u32x4*)(row + (int64_t)i * 16);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = unpack16<BF>(j & 1 ? a[j / 2] >> 16 : a[j / 2] & 0xffffu);
-    }
+    for (int j = 0; j < 8; ++j) v[j] = j < 4 ? a[j % 4] : b[j % 4];
   } else {
+    const u32x4 a = *(const typename Unaligned<VEC ? 16 : 2, u32x4>::type*)(row + at * 2);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = i + j * step;
-      v[j] = e >= d ? 0.0f
-             : f32  ? *(const float*)(row + (int64_t)e * 4)
-                    : unpack16<BF>(*(const uint16_t*)(row + (int64_t)e * 2));
-    }
+    for (int j = 0; j < 8; ++j) v[j] = unpack16<BF>(j & 1 ? a[j / 2] >> 16 : a[j / 2] & 0xffffu);
   }
 }
 
 template <bool BF, bool VEC>
-__device__ __forceinline__ void store8(uint8_t* row, bool f32, int i, int step, int d, const float (&v)[8]) {
-  if constexpr (VEC) {
-    if (8 * i >= d) return;
-    if (f32) {
-      *(f32x4*)(row + (int64_t)i * 32) = f32x4{v[0], v[1], v[2], v[3]};
-      *(f32x4*)(row + (int64_t)i * 32 + 16) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-      *(u32x4*)(row + (int64_t)i * 16) = u32x4{pack16<BF>(v[0], v[1]), pack16<BF>(v[2], v[3]),
-                                                pack16<BF>(v[4], v[5]), pack16<BF>(v[6], v[7])};
-    }
-  } else {
+__device__ __forceinline__ void store8(uint8_t* row, bool f32, int i, int d, const float (&v)[8]) {
+  const int64_t at = (int64_t)i * 8;
+  if (VEC ? 8 * i >= d : 8 * i + 8 > d) {
+    if (VEC) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int e = i + j * step;
-      if (e >= d) continue;
-      if (f32) *(float*)(row + (int64_t)e * 4) = v[j];
-      else *(uint16_t*)(row + (int64_t)e * 2) = (uint16_t)pack16<BF>(v[j], 0.0f);
+      if (at + j >= d) continue;
+      if (f32) *(float*)(row + (at + j) * 4) = v[j];
+      else *(uint16_t*)(row + (at + j) * 2) = (uint16_t)pack16<BF>(v[j], 0.0f);
     }
+  } else if (f32) {
+    typedef typename Unaligned<VEC ? 16 : 4, f32x4>::type Four;
+    *(Four*)(row + at * 4) = f32x4{v[0], v[1], v[2], v[3]};
+    *(Four*)(row + at * 4 + 16) = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+    *(typename Unaligned<VEC ? 16 : 2, u32x4>::type*)(row + at * 2) =
+        u32x4{pack16<BF>(v[0], v[1]), pack16<BF>(v[2], v[3]), pack16<BF>(v[4], v[5]), pack16<BF>(v[6], v[7])};
   }
 }
 
@@ -166,35 +165,43 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
   const int threads = waves * 64, tid = waves == 1 ? threadIdx.x & 63 : threadIdx.x;
   RowSum sum = {red, wide, waves, wave, 0};
   const bool x32 = VEC ? X32 : A.x32, y32 = VEC ? Y32 : A.y32, o32 = VEC ? O32 : A.o32;
-  auto at = [&](int k) { return VEC ? tid + k * threads : tid + k * 8 * threads; };
+  auto at = [&](int k) { return tid + k * threads; };
 
-  float x[V][8], y[V][8];
+  // x beside y from the start; of long rows x when y's sums are known, in y's registers
+  constexpr bool kEarly = V <= 2;
+  float x[V][8], y[kEarly ? V : 1][8];
   bool in[V][8];
-#pragma unroll
-  for (int k = 0; k < V; ++k) load8<BF, VEC>(A.x + row * A.x_row, x32, at(k), threads, A.d, x[k]);
 #pragma unroll
   for (int k = 0; k < V; ++k)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) in[k][j] = (VEC ? 8 * at(k) : at(k) + j * threads) < A.d;
-  if (A.y) {
+    for (int j = 0; j < 8; ++j) in[k][j] = 8 * at(k) + (VEC ? 0 : j) < A.d;
+  if (kEarly || !A.y) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) load8<BF, VEC>(A.y + row * A.y_row, y32, at(k), threads, A.d, y[k]);
+    for (int k = 0; k < V; ++k) load8<BF, VEC>(A.x + row * A.x_row, x32, at(k), A.d, x[k]);
+  }
+  if (A.y) {
+    float (&t)[V][8] = *[&] {
+      if constexpr (kEarly) return &y;
+      else return &x;
+    }();
+#pragma unroll
+    for (int k = 0; k < V; ++k) load8<BF, VEC>(A.y + row * A.y_row, y32, at(k), A.d, t[k]);
     if (A.post) {
-      const float2 st = statistics<V>(A, y, in, sum);
+      const float2 st = statistics<V>(A, t, in, sum);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[k][j] = (y[k][j] - st.x) * st.y;
+        for (int j = 0; j < 8; ++j) t[k][j] = (t[k][j] - st.x) * st.y;
         float w[8];
         if (A.post_weight) {
-          load8<BF, VEC>(A.post_weight, A.w32, at(k), threads, A.d, w);
+          load8<BF, VEC>(A.post_weight, A.w32, at(k), A.d, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[k][j] *= w[j];
+          for (int j = 0; j < 8; ++j) t[k][j] *= w[j];
         }
         if (A.post_bias) {
-          load8<BF, VEC>(A.post_bias, A.w32, at(k), threads, A.d, w);
+          load8<BF, VEC>(A.post_bias, A.w32, at(k), A.d, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[k][j] += w[j];
+          for (int j = 0; j < 8; ++j) t[k][j] += w[j];
         }
       }
     }
@@ -202,17 +209,19 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
     for (int k = 0; k < V; ++k) {
       if (A.gate) {
         float g[8];
-        load8<BF, VEC>(A.gate + row * A.gate_row, A.w32, at(k), threads, A.d, g);
+        load8<BF, VEC>(A.gate + row * A.gate_row, A.w32, at(k), A.d, g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[k][j] *= g[j];
+        for (int j = 0; j < 8; ++j) t[k][j] *= g[j];
       }
+      float late[8];
+      if constexpr (!kEarly) load8<BF, VEC>(A.x + row * A.x_row, x32, at(k), A.d, late);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[k][j] = fmaf(A.scale, in[k][j] ? y[k][j] : 0.0f, x[k][j]);
+      for (int j = 0; j < 8; ++j) x[k][j] = fmaf(A.scale, in[k][j] ? t[k][j] : 0.0f, kEarly ? x[k][j] : late[j]);
     }
   }
   if (A.x_out) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) store8<BF, VEC>(A.x_out + row * A.x_out_row, x32, at(k), threads, A.d, x[k]);
+    for (int k = 0; k < V; ++k) store8<BF, VEC>(A.x_out + row * A.x_out_row, x32, at(k), A.d, x[k]);
   }
   if (!A.out) return;
   const float2 st = statistics<V>(A, x, in, sum);
@@ -222,16 +231,16 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
     for (int j = 0; j < 8; ++j) x[k][j] = (x[k][j] - st.x) * st.y;
     float w[8];
     if (A.weight) {
-      load8<BF, VEC>(A.weight, A.w32, at(k), threads, A.d, w);
+      load8<BF, VEC>(A.weight, A.w32, at(k), A.d, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[k][j] *= w[j];
     }
     if (A.bias) {
-      load8<BF, VEC>(A.bias, A.w32, at(k), threads, A.d, w);
+      load8<BF, VEC>(A.bias, A.w32, at(k), A.d, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[k][j] += w[j];
     }
-    store8<BF, VEC>(A.out + row * A.out_row, o32, at(k), threads, A.d, x[k]);
+    store8<BF, VEC>(A.out + row * A.out_row, o32, at(k), A.d, x[k]);
   }
 }
 
@@ -245,11 +254,12 @@ hipError_t launch_rows(const NormArgs& A, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <bool BF, bool X32, bool Y32, bool O32>
+template <bool BF, bool X32, bool Y32, bool O32, bool VEC>
 hipError_t launch_typed(const NormArgs& A, hipStream_t stream) {
-  if (A.d <= 1024) return launch_rows<BF, X32, Y32, O32, 1, true>(A, stream);
-  if (A.d <= 16384) return launch_rows<BF, X32, Y32, O32, 2, true>(A, stream);
-  return launch_rows<BF, X32, Y32, O32, 8, true>(A, stream);
+  if (A.d <= 1024) return launch_rows<BF, X32, Y32, O32, 1, VEC>(A, stream);
+  if (A.d <= 16384) return launch_rows<BF, X32, Y32, O32, 2, VEC>(A, stream);
+  if (A.d <= 32768) return launch_rows<BF, X32, Y32, O32, 4, VEC>(A, stream);
+  return launch_rows<BF, X32, Y32, O32, 8, VEC>(A, stream);
 }
 
 }  // namespace
@@ -290,11 +300,11 @@ hipError_t launch_residual_norm(const m2c_norm_desc* D, const void* x, const voi
   const auto flag = [](bool b, auto f) { return b ? f(std::true_type()) : f(std::false_type()); };
   return flag(bf, [&](auto b) {
     constexpr bool BF = decltype(b)::value;
-    if (!vec) return launch_rows<BF, false, false, false, 8, false>(A, stream);
+    if (!vec) return launch_typed<BF, false, false, false, false>(A, stream);
     return flag(A.x32, [&](auto x32) {
       return flag(A.y32, [&](auto y32) {
         return flag(A.o32, [&](auto o32) {
-          return launch_typed<BF, decltype(x32)::value, decltype(y32)::value, decltype(o32)::value>(A, stream);
+          return launch_typed<BF, decltype(x32)::value, decltype(y32)::value, decltype(o32)::value, true>(A, stream);
         });
       });
     });
