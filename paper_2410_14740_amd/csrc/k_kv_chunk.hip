@@ -48,8 +48,8 @@ struct ChunkArgs : RowArgs {
 
 namespace {
 
-// Values lie in LDS as in the attention of prompts, and a bit further apart: where a
-// wave writes two rows at once, one's 16-byte chunks are even and the other's odd.
+// Values lie in LDS as in the attention of prompts, but that odd rows (of 64: the
+// second two of four) swap neighbouring chunks, for the writes of codes.
 template <int D>
 __device__ __forceinline__ int swz_values(int row) {
   return D == 128 ? (row & 3) << 2 | (row & 1) : ((row >> 1) & 1) * 5;
@@ -427,9 +427,14 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], -up);
     };
-    // A wave's rows of a tile are 16 wave .. + 15: lane i takes chunk i % kCodeChunks
-    // of rows i / kCodeChunks, + 64 / kCodeChunks.
-    const int c_row = lane / kCodeChunks, c_chunk = lane % kCodeChunks;
+    // A wave's rows of a tile are 16 wave .. + 15. A load covers 1024 bytes of them, 16
+    // codes a lane, which become two chunks of 16 bytes in LDS. LDS takes 128 bytes of
+    // a write at a time, eight lanes': four of one row, whose chunks are even, and four
+    // of another, whose are odd by the swizzle (all eight of one row: half as fast).
+    const int c_row = D == 128 ? (lane >> 4) * 2 + (lane >> 2 & 1)
+                               : (lane >> 4) * 4 + (lane >> 2 & 1) * 2 + (lane >> 3 & 1);
+    const int c_chunk = D == 128 ? (lane >> 3 & 1) * 4 + (lane & 3) : lane & 3;
+    const int c_at = c_row * D + c_chunk * 16;
     u32x4 rk[CL], rv[CL];
     auto load_codes = [&](int t, int page) {  // a page of -1 loads zeros
       const int64_t at = (((int64_t)max(page, 0) << shift) + (((ta + t) * kTileK + 16 * wave) & (BT - 1))) * D;
@@ -437,9 +442,9 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
       const auto kr = __builtin_amdgcn_make_buffer_rsrc(P.C.k_codes + at, 0, bytes, 0x00020000);
       const auto vr = __builtin_amdgcn_make_buffer_rsrc(P.C.v_codes + at, 0, bytes, 0x00020000);
 #pragma unroll
-      for (int i = 0; i < CL; ++i) rk[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, lane * 16 + i * 1024, 0, 0));
+      for (int i = 0; i < CL; ++i) rk[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, c_at + i * 1024, 0, 0));
 #pragma unroll
-      for (int i = 0; i < CL; ++i) rv[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, lane * 16 + i * 1024, 0, 0));
+      for (int i = 0; i < CL; ++i) rv[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, c_at + i * 1024, 0, 0));
     };
     auto write_codes = [&](int t, const u32x4 (&x)[CL], bool values) {
 #pragma unroll
