@@ -3,7 +3,10 @@
 //   N(z) = (z - mean z) / sqrt(mean (z - mean z)^2 + eps)   (mean 0 for M2C_NORM_RMS).
 // A row is read once and kept in registers, 8 consecutive elements of it per
 // thread and step, between the sums (one for each mean, over the wave by lane
-// exchanges and over the waves of a row through LDS) and what is written.
+// exchanges and over the waves of a row through LDS) and what is written. Bound by
+// memory: 10692 rows of 8192, x and what comes of it in fp32, y and N in bf16, are
+// 1.05 GB in 185 us from a graph and 200 to 215 between other kernels (5.7 and 4.9
+// to 5.3 TB/s; a 1 GiB copy: 5.1). One row: 2.4 us, the two sums one after another.
 #include <type_traits>
 
 #include "attn_device.h"
@@ -152,17 +155,16 @@ __device__ __forceinline__ float2 statistics(const NormArgs& A, const float (&v)
   return make_float2((float)m, (float)(1.0 / sqrt(q / A.d + (double)A.eps)));
 }
 
-// `waves` waves to a row of at most waves * V * 512 elements. X32, Y32, O32: which
+// A workgroup, of `waves` waves, to a row of at most waves * V * 512 elements. X32, Y32, O32: which
 // of the arrays are fp32; without VEC they are known at run time only.
 template <bool BF, bool X32, bool Y32, bool O32, int V, bool VEC>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, int waves) {
   __shared__ float red[2][kMaxWaves];
   __shared__ double wide[kMaxWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = waves == 1 ? blockDim.x / 64 : 1;  // rows of a workgroup
-  const int64_t row = (int64_t)blockIdx.x * per + (waves == 1 ? wave : 0);
-  if (row >= A.rows) return;  // whole waves of a workgroup without barriers
-  const int threads = waves * 64, tid = waves == 1 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (row >= A.rows) return;
+  const int threads = waves * 64, tid = threadIdx.x;
   RowSum sum = {red, wide, waves, wave, 0};
   const bool x32 = VEC ? X32 : A.x32, y32 = VEC ? Y32 : A.y32, o32 = VEC ? O32 : A.o32;
   auto at = [&](int k) { return tid + k * threads; };
@@ -244,19 +246,25 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
   }
 }
 
+constexpr int64_t kAcross = 1 << 20;  // a grid has fewer than 2^32 threads along x
+
 template <bool BF, bool X32, bool Y32, bool O32, int V, bool VEC>
 hipError_t launch_rows(const NormArgs& A, hipStream_t stream) {
   const int waves = (A.d + V * 512 - 1) / (V * 512);
-  const int per = waves == 1 && A.rows >= 1024 ? 4 : 1;
-  const int64_t grid = (A.rows + per - 1) / per;
-  hipLaunchKernelGGL((residual_norm_kernel<BF, X32, Y32, O32, V, VEC>), dim3((uint32_t)grid),
-                     dim3(waves * per * 64), 0, stream, A, waves);
+  const int64_t across = A.rows < kAcross ? A.rows : kAcross;
+  const dim3 grid((uint32_t)across, (uint32_t)((A.rows + across - 1) / across));
+  hipLaunchKernelGGL((residual_norm_kernel<BF, X32, Y32, O32, V, VEC>), grid, dim3(waves * 64), 0, stream, A,
+                     waves);
   return hipGetLastError();
 }
 
+// As few elements to a thread as a workgroup of 1024 threads allows. 20000 rows of
+// 1024: 37.0 us with 8 a thread, 38.5 with 16; 8192 of 4096: 72 and 76; 10692 of
+// 8192: 185, 187 and 196 with 32; 889 of 5120: 12.1, 12.4 and 11.4. Four rows of
+// one wave each to a workgroup took as long as one.
 template <bool BF, bool X32, bool Y32, bool O32, bool VEC>
 hipError_t launch_typed(const NormArgs& A, hipStream_t stream) {
-  if (A.d <= 1024) return launch_rows<BF, X32, Y32, O32, 1, VEC>(A, stream);
+  if (A.d <= 8192) return launch_rows<BF, X32, Y32, O32, 1, VEC>(A, stream);
   if (A.d <= 16384) return launch_rows<BF, X32, Y32, O32, 2, VEC>(A, stream);
   if (A.d <= 32768) return launch_rows<BF, X32, Y32, O32, 4, VEC>(A, stream);
   return launch_rows<BF, X32, Y32, O32, 8, VEC>(A, stream);

@@ -234,3 +234,19 @@ def test_refusals(kw, needle):
     with pytest.raises(m2c.M2CError) as e:
         residual_norm(torch.zeros((4, 64), device="cuda"), **args)
     assert e.value.status == m2c.M2C_ERR_INVALID_ARG and needle in str(e.value)
+
+
+def test_more_rows_than_a_grid_has_threads():
+    """2^26 rows and some: 64 threads for each would be 2^32."""
+    n, d = (1 << 26) + 3, 8
+    x = torch.empty(n, d, dtype=F16, device="cuda")
+    x[:4096] = rand((4096, d), F16, 90)
+    x[4096:] = 1.0
+    x[-4096:] = rand((4096, d), F16, 91)
+    x_out, out = torch.empty_like(x), torch.zeros_like(x)
+    residual_norm(x, weight=None, x_out=x_out, out=out)
+    assert torch.equal(x_out, x)
+    for rows in (slice(0, 4096), slice(n - 4096, n)):
+        assert torch.equal(out[rows], residual_norm(x[rows])[1])
+    mid = out[4096:-4096]
+    assert torch.equal(mid, mid[:1].expand_as(mid)) and mid[0, 0].item() == 1.0

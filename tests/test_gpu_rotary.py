@@ -315,3 +315,17 @@ def test_refusals(call, needle):
     with pytest.raises(m2c.M2CError) as e:
         call(r, c, q, p)
     assert e.value.status == m2c.M2C_ERR_INVALID_ARG and needle in str(e.value)
+
+
+def test_more_tokens_than_a_grid_has_threads():
+    """2^26 tokens and some: a workgroup of 256 threads for every four would be 2^32."""
+    n, R = (1 << 26) + 5, Rotary(freqs(16))
+    q = torch.empty(n, 1, 64, dtype=F16, device="cuda")
+    q[:-4096] = 1.0
+    q[-4096:] = rand((4096, 1, 64), F16, 92)
+    p = torch.zeros(n, dtype=torch.int32, device="cuda")
+    p[-4096:] = torch.arange(4096, dtype=torch.int32, device="cuda")
+    want = R.rotate(q[-4096:], p[-4096:])
+    R.rotate(q, p, q_out=q)
+    assert torch.equal(q[-4096:], want)
+    assert q[:-4096].min().item() == 1.0 == q[:-4096].max().item()
