@@ -507,3 +507,49 @@ def test_refusals(call, needle):
     with pytest.raises(m2c.M2CError) as e:
         call(c, torch.zeros((6, 4, 64), dtype=F16, device="cuda"), starts([2, 4]))
     assert e.value.status == m2c.M2C_ERR_INVALID_ARG and needle in str(e.value)
+
+
+@pytest.mark.parametrize("new", [False, True])
+def test_pages_past_32_bits(new):
+    """Pages whose byte offsets do not fit 32 bits."""
+    say(f"chunk pages past 32 bits {new}")
+    hk, d, n_pages = 2, 128, (1 << 19) + 64  # 8 KB of codes a page
+    c = KVCache(1, hk, d, 8, n_pages=n_pages, dtype=F16)
+    c.table.copy_(torch.arange(n_pages - 16, n_pages, dtype=torch.int32, device="cuda").flip(0).view_as(c.table))
+    c.append(rand((500, hk, d), F16, 2), rand((500, hk, d), F16, 3), cu=starts([500]))
+    q, k, v = rand((37, 4, d), F16, 4), rand((37, hk, d), F16, 5), rand((37, hk, d), F16, 6)
+    if not new:
+        k = v = None
+    out, lse = c.attend_chunk(q, starts([37]), k, v, return_lse=True)
+    c.check()
+    check(c, q, starts([37]), k, v, out, lse)
+
+
+def test_a_full_cache():
+    """A sequence at the end of its blocks, and a chunk behind it that would not fit."""
+    say("chunk full cache")
+    c = make(2, 2, 64, 64, BF16, [256, 255])
+    q, k, v = rand((80, 4, 64), BF16, 2), rand((80, 2, 64), BF16, 3), rand((80, 2, 64), BF16, 4)
+    cu = starts([70, 10])
+    for kv in ((k, v), (None, None)):
+        out, lse = c.attend_chunk(q, cu, *kv, return_lse=True)
+        check(c, q, cu, *kv, out, lse)
+    c.check()
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, whose rows are cut, over one cache, as one after another."""
+    say("chunk two at once")
+    c = make(2, 2, 128, 64, F16, [6000, 900])
+    cu, calls = starts([20, 9]), []
+    for i in range(2):
+        q, k, v = (rand((29, h, 128), F16, 10 * i + j) for j, h in enumerate((8, 2, 2)))
+        calls.append((q, k, v, c.attend_chunk(q, cu, k, v)))
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[c.attend_chunk(*call[:1], cu, *call[1:3], stream=s) for s, call in zip(sides, calls)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for out, call in zip(pair, calls):
+            assert torch.equal(out, call[3])
+    check(c, calls[0][0], cu, calls[0][1], calls[0][2], calls[0][3], None)

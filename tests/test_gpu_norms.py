@@ -250,3 +250,15 @@ def test_more_rows_than_a_grid_has_threads():
         assert torch.equal(out[rows], residual_norm(x[rows])[1])
     mid = out[4096:-4096]
     assert torch.equal(mid, mid[:1].expand_as(mid)) and mid[0, 0].item() == 1.0
+
+
+def test_rows_far_apart():
+    """Rows whose byte offsets do not fit 32 bits."""
+    d, step = 264, (1 << 30) + 8
+    buf = torch.empty(2 * step + d, dtype=F16, device="cuda")
+    x, y = buf.as_strided((3, d), (step, 1)), rand((3, d), F16, 95)
+    x.copy_(rand((3, d), F16, 94))
+    want = residual_norm(x.contiguous(), y)
+    out = torch.empty_like(buf).as_strided((3, d), (step, 1))
+    got = residual_norm(x, y, x_out=x, out=out)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -329,3 +329,14 @@ def test_more_tokens_than_a_grid_has_threads():
     R.rotate(q, p, q_out=q)
     assert torch.equal(q[-4096:], want)
     assert q[:-4096].min().item() == 1.0 == q[:-4096].max().item()
+
+
+def test_heads_far_apart():
+    """Heads whose byte offsets do not fit 32 bits, turned in place."""
+    n, R, step = 9, Rotary(freqs(64)), (1 << 30) + 64
+    buf = torch.empty(2 * step + n * 64, dtype=F16, device="cuda")
+    q = buf.as_strided((n, 3, 64), (64, step, 1))
+    q.copy_(rand((n, 3, 64), F16, 93))
+    p = torch.arange(n, dtype=torch.int32, device="cuda")
+    want = R.rotate(q.contiguous(), p)
+    assert torch.equal(R.rotate(q, p, q_out=q), want)
