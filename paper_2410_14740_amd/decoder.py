@@ -34,6 +34,21 @@ from .attention import KVCache, Rotary, prompt_attention
 from .norms import residual_norm
 
 
+def norm(x):
+    """Root-mean-square norm of fp32 rows, as fp16 rows, in torch's operations."""
+    return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)).half()
+
+
+def rotate(x, pos):
+    """Rotary position embedding of x [tokens][heads][dim] at positions pos [tokens],
+    in torch's operations (any width; angles in fp32)."""
+    half = x.shape[-1] // 2
+    freq = 10000.0 ** (-torch.arange(half, device=x.device, dtype=torch.float32) / half)
+    a = pos.float()[:, None, None] * freq
+    lo, hi = x[..., :half].float(), x[..., half:].float()
+    return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1).to(x.dtype)
+
+
 def rotary(dim, device="cuda"):
     """The rotation of a head of `dim` elements whose pairs turn once in 2 pi 10000^(2 i / dim) positions."""
     half = dim // 2
@@ -78,15 +93,22 @@ class DecoderLayer:
         self.cache = KVCache(n_seqs, n_kv_heads, self.dim, -(-max_tokens // block_tokens), block_tokens)
         self.tiers = torch.empty((ffn.desc.max_batch, ffn.desc.d_ff), dtype=torch.uint8, device="cuda")
 
-    def project(self, x):
-        """Queries, keys and values of rows of the stream, not rotated yet."""
+    def project(self, x, pos=None):
+        """Queries, keys and values of rows of the stream; queries and keys rotated
+        by positions pos [rows] if given."""
         h, g = self.n_heads, self.n_kv_heads
         rows = (residual_norm(x)[1] @ self.wqkv).view(x.shape[0], h + 2 * g, self.dim)
-        return rows[:, :h], rows[:, h:h + g], rows[:, h + g:]
+        q, k, v = rows[:, :h], rows[:, h:h + g], rows[:, h + g:]
+        if pos is not None:
+            self.rotary.rotate(q, _places(pos), k=k, q_out=q, k_out=k)
+        return q, k, v
 
-    def feed_forward(self, x, attended):
-        """x += attended Wo, x += FFN(norm(x)), max_batch rows at a time."""
-        _, rows = residual_norm(x, attended.reshape(x.shape[0], -1) @ self.wo, x_out=x)
+    def feed_forward(self, x, attended=None):
+        """x += attended Wo if given, x += FFN(norm(x)), max_batch rows at a time."""
+        if attended is None:
+            _, rows = residual_norm(x)
+        else:
+            _, rows = residual_norm(x, attended.reshape(x.shape[0], -1) @ self.wo, x_out=x)
         for a in range(0, x.shape[0], self.ffn.desc.max_batch):
             part = rows[a:a + self.ffn.desc.max_batch]
             n, L = part.shape[0], self.ffn
@@ -100,13 +122,13 @@ class DecoderLayer:
         """A chunk of every sequence: rows x are lens[b] tokens of sequence b,
         whose cache holds before[b]. Host lists; x is updated in place."""
         pos = torch.cat([torch.arange(p, p + n, dtype=torch.int32, device="cuda") for n, p in zip(lens, before)])
-        q, k, v = self.project(x)
         cu = _starts(lens)
         if not any(before):
+            q, k, v = self.project(x)
             q, k = self.cache.append_rotated(self.rotary, k, v, pos, q=q, cu=cu, k_out=True)
             out = prompt_attention(q, k, v, cu, max_q=max(lens))
         else:
-            self.rotary.rotate(q, pos, k=k, q_out=q, k_out=k)
+            q, k, v = self.project(x, pos)
             out = self.attend(q, k, v, cu, lens, before)
             self.cache.append(k, v, cu=cu)
         self.feed_forward(x, out)
@@ -124,10 +146,10 @@ class DecoderLayer:
         return prompt_attention(q, keys, values, cu, cu_k, max_q=max(lens))
 
     def decode(self, x, pos, max_len):
-        """One token per sequence at positions pos (int32 tensor); max_len: the
+        """One token per sequence at positions pos (integer tensor); max_len: the
         longest sequence afterwards. x is updated in place."""
         q, k, v = self.project(x)
-        q, _ = self.cache.append_rotated(self.rotary, k, v, pos, q=q)
+        q, _ = self.cache.append_rotated(self.rotary, k, v, _places(pos), q=q)
         out = self.cache.attend(q, max_len=max_len, track=self.budget > 0)
         self.feed_forward(x, out)
 
@@ -136,6 +158,11 @@ class DecoderLayer:
         `recent` of those that may (as many as the budget holds)."""
         first = min(first, self.budget)
         self.cache.evict(self.budget, first, min(recent, self.budget - first))
+
+
+def _places(pos):
+    """Positions as the library takes them."""
+    return pos.to(torch.int32).contiguous()
 
 
 def _starts(lens):
