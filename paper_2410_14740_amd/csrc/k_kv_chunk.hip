@@ -413,6 +413,9 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
     }
     // u of bf16 caches: 2^-20 of the first block's scale that is not 0, or 2^-100 of
     // what O has by then, and a larger one should a later scale be 2^40 times as large.
+    // In a larger unit every x + g so far is as much less, and so is m, which later
+    // weights are to be measured by; l, a sum of 2^(x - m), grows. Where l would pass
+    // 2^100 (a sum of blocks 2^-80 of the new one's size) O takes the rest.
     bool unit_set = !BF;
     auto set_unit = [&](int e) __attribute__((always_inline)) {  // for a scale in [2^(e - 1), 2^e)
       int up = e - 20 - u;
@@ -431,10 +434,14 @@ __global__ void __launch_bounds__(kWaves * 64, 2) chunk_attention_kernel(const C
         unit_set = true;
       }
       u += up;
+      const int most = 227 - (int)(__float_as_uint(max_xor32(l)) >> 23);  // the row's l stays below 2^101
+      const int by = max(0, min(up, most));
+      m -= (float)by;
+      l = ldexpf(l, by);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], -up);
+        for (int r = 0; r < 16; ++r) o[dt][r] = ldexpf(o[dt][r], by - up);
     };
     // A wave's rows of a tile are 16 wave .. + 15. A load covers 1024 bytes of them, 16
     // codes a lane, which become two chunks of 16 bytes in LDS. LDS takes 128 bytes of
