@@ -102,3 +102,16 @@ def test_rows_cut_along_the_keys(parts):
     say(f"chunk units cut {parts}")
     c = cache(64, 32, parts)
     attend(c, 3, 64, max_q=3, max_len=int(c.len[0]))
+
+
+@pytest.mark.parametrize("parts", [
+    [(1, 1.0, -30), (1, 2.0 ** 39, 0), (500, 0.0, -20)], [(1, 1.0, -30), (1, 2.0 ** 30, 0), (500, 0.0, -24)],
+    [(1, 1.0, -30), (1, 2.0 ** 39, 0), (500, 2.0 ** -38, -20)]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_small_weights_of_small_blocks(parts, d):
+    """16000 keys of weights 2^-20 or 2^-24, whose values are zeros or small, after a
+    large block that has the rest: they are 1.5% or 0.1% of the sum of weights."""
+    say(f"chunk units small {parts} {d}")
+    c = cache(d, 32, parts)
+    attend(c, 1, d)
+    attend(c, 2, d, max_q=2, max_len=int(c.len[0]))
