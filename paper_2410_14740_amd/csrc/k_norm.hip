@@ -110,11 +110,18 @@ struct RowSum {
   }
 };
 
-// mean and 1 / sqrt(mean square + eps) of a row in registers. Sums are fp32;
-// where they leave its range (a row of numbers near the largest or smallest, or
-// of zeros) they are taken again in 64 bits.
+// What takes a row in registers to N of it: z becomes (z size - mean) f. Sums are
+// fp32; where they leave its range (a row of numbers near the largest or smallest,
+// or of zeros) they are taken again in 64 bits, and the row is brought near 1 by a
+// power of two first, as z - mean or 1 / sqrt may leave fp32 too.
+struct Norm {
+  float size, mean, f;
+};
+
+__device__ __forceinline__ int exponent_of(double v) { return (int)(__double_as_longlong(v) >> 52 & 0x7ff) - 1023; }
+
 template <int V>
-__device__ __forceinline__ float2 statistics(const NormArgs& A, const float (&v)[V][8], const bool (&in)[V][8],
+__device__ __forceinline__ Norm statistics(const NormArgs& A, const float (&v)[V][8], const bool (&in)[V][8],
                                              RowSum& sum) {
   float mean = 0.0f;
   if (A.layer) {
@@ -134,7 +141,7 @@ __device__ __forceinline__ float2 statistics(const NormArgs& A, const float (&v)
       s = fmaf(c, c, s);
     }
   s = sum.add(s);
-  if (s > 0x1p-80f && s < 0x1p120f) return make_float2(mean, __frsqrt_rn(fmaf(s, A.inv_d, A.eps)));
+  if (s > 0x1p-80f && s < 0x1p120f) return {1.0f, mean, __frsqrt_rn(fmaf(s, A.inv_d, A.eps))};
   double m = 0.0;
   if (A.layer) {
 #pragma unroll
@@ -151,8 +158,11 @@ __device__ __forceinline__ float2 statistics(const NormArgs& A, const float (&v)
       const double c = in[k][j] ? (double)v[k][j] - m : 0.0;
       q = fma(c, c, q);
     }
-  q = sum.add(q);
-  return make_float2((float)m, (float)(1.0 / sqrt(q / A.d + (double)A.eps)));
+  const double rms = sqrt(sum.add(q) / A.d + (double)A.eps);
+  // the mean of a row of nearly equal numbers, far larger than rms, stays below 2^121
+  const int e = max(min(max(exponent_of(rms), -126), 126), exponent_of(m) - 120);
+  const double size = rms > 0.0 && rms < 0x1p200 ? ldexp(1.0, -e) : 1.0;
+  return {(float)size, (float)(m * size), (float)(1.0 / (rms * size))};
 }
 
 // A workgroup, of `waves` waves, to a row of at most waves * V * 512 elements. X32, Y32, O32: which
@@ -189,11 +199,11 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
 #pragma unroll
     for (int k = 0; k < V; ++k) load8<BF, VEC>(A.y + row * A.y_row, y32, at(k), A.d, t[k]);
     if (A.post) {
-      const float2 st = statistics<V>(A, t, in, sum);
+      const Norm st = statistics<V>(A, t, in, sum);
 #pragma unroll
       for (int k = 0; k < V; ++k) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[k][j] = (t[k][j] - st.x) * st.y;
+        for (int j = 0; j < 8; ++j) t[k][j] = fmaf(t[k][j], st.size, -st.mean) * st.f;
         float w[8];
         if (A.post_weight) {
           load8<BF, VEC>(A.post_weight, A.w32, at(k), A.d, w);
@@ -226,11 +236,11 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(const NormArgs A, i
     for (int k = 0; k < V; ++k) store8<BF, VEC>(A.x_out + row * A.x_out_row, x32, at(k), A.d, x[k]);
   }
   if (!A.out) return;
-  const float2 st = statistics<V>(A, x, in, sum);
+  const Norm st = statistics<V>(A, x, in, sum);
 #pragma unroll
   for (int k = 0; k < V; ++k) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[k][j] = (x[k][j] - st.x) * st.y;
+    for (int j = 0; j < 8; ++j) x[k][j] = fmaf(x[k][j], st.size, -st.mean) * st.f;
     float w[8];
     if (A.weight) {
       load8<BF, VEC>(A.weight, A.w32, at(k), A.d, w);
