@@ -122,21 +122,22 @@ struct TurnAppend {
 // One block of one sequence and key/value head. Thread t holds chunk t % (D/8)
 // of tokens t / (D/8), + 256 / (D/8), ..
 // Keys that turn by their positions are stored in k_out as well, if there is one,
-// and workgroups past the blocks turn the queries.
+// and workgroups past the blocks turn the queries. across: blocks of a head along x.
 template <bool BF, int D, int BT, class How>
 __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32_t* seqs, int n,
                                                      const int32_t* cu, int64_t total,
                                                      const int32_t* pos, const uint8_t* k,
                                                      const uint8_t* v, int64_t k_tok, int64_t k_head,
                                                      int64_t v_tok, int64_t v_head,
-                                                     const How R) {
+                                                     int across, const How R) {
   constexpr int CH = D / 8, TP = 256 / CH;  // chunks of a token, tokens a pass of 256 threads takes
   constexpr int NP = BT / TP;
   __shared__ uint32_t mags[2][4];
   if constexpr (How::kTurns) {
     __shared__ __align__(16) float2 cs[kTurnTokens][64];
-    if ((int64_t)blockIdx.x >= R.blocks) {
-      const int i = (int)((int64_t)blockIdx.x - R.blocks), g = i / R.parts, part = i - g * R.parts;
+    const int64_t block = (int64_t)blockIdx.y * across * C.n_kv_heads + blockIdx.x;
+    if (block >= R.blocks) {
+      const int i = (int)(block - R.blocks), g = i / R.parts, part = i - g * R.parts;
       // rows of no sequence stay as they are
       const int64_t lo = cu ? clamp64(cu[0], 0, total) : 0, hi = cu ? clamp64(cu[n], lo, total) : total;
       const int64_t tok0 = lo + (int64_t)g * kTurnTokens;
@@ -147,7 +148,8 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
       return;
     }
   }
-  const int x = blockIdx.x / C.n_kv_heads, head = blockIdx.x - x * C.n_kv_heads, tid = threadIdx.x;
+  const int column = blockIdx.x / C.n_kv_heads, head = blockIdx.x - column * C.n_kv_heads, tid = threadIdx.x;
+  const int x = blockIdx.y * across + column;
   int b = x, item = 0, items = 1;
   int64_t row0 = b;
   int nb = 1;
@@ -161,6 +163,8 @@ __global__ void __launch_bounds__(256) append_kernel(const KvView C, const int32
     item = (int)(x - s0);
     items = (int)(item_start(row1, b + 1, BT, 2) - s0);
     if (item < 0 || item >= items) return;  // past the last sequence's, or starts that do not ascend
+  } else if (x >= n) {
+    return;
   }
   if (nb == 0) return;  // nothing of this sequence changes
   const int s = seqs ? seqs[b] : b;
@@ -385,6 +389,8 @@ hipError_t by_shape(const KvView& C, F f) {
 
 namespace {
 
+constexpr int64_t kAcross = 1 << 20;
+
 template <class How>
 hipError_t append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu, int64_t total,
                   const int32_t* pos, const void* k, const void* v, const int64_t* ks, const int64_t* vs,
@@ -398,12 +404,15 @@ hipError_t append(const KvView& C, const int32_t* seqs, int n, const int32_t* cu
     R.parts = (int)std::min<int64_t>(std::max<int64_t>(512 / groups, 1), (R.Q.heads + 7) / 8);
     grid += groups * R.parts;
   }
-  if (grid > UINT32_MAX / 256) return hipErrorInvalidValue;  // of threads a grid has fewer than 2^32
+  // along x a grid has fewer than 2^32 threads: y as well where that is not enough
+  const bool flat = grid * 256 <= UINT32_MAX;
+  const int64_t across = flat ? items : kAcross / C.n_kv_heads;  // heads: 1024 at most
+  const int64_t width = flat ? grid : across * C.n_kv_heads, rows = (grid + width - 1) / width;
   const hipError_t e = by_shape(C, [&](auto bf, auto d, auto bt) {
     hipLaunchKernelGGL((append_kernel<decltype(bf)::value, decltype(d)::value, decltype(bt)::value, How>),
-                       dim3((uint32_t)grid), dim3(256), 0, stream, C, seqs, n, cu,
+                       dim3((uint32_t)width, (uint32_t)rows), dim3(256), 0, stream, C, seqs, n, cu,
                        total, pos, (const uint8_t*)k, (const uint8_t*)v, ks[0] * 2, ks[1] * 2,
-                       vs[0] * 2, vs[1] * 2, R);
+                       vs[0] * 2, vs[1] * 2, (int)across, R);
     return hipGetLastError();
   });
   if (e != hipSuccess || !cu) return e;
