@@ -679,7 +679,8 @@ m2c_status m2c_kv_attend(const m2c_kv_cache* cache, const int32_t* seqs, int32_t
 
 /* Bytes of the workspace with which m2c_kv_attend_chunk with the same arguments
  * splits the queries that see many more keys than the others along them (0 where
- * it would split none), or -1. */
+ * it would split none: always for n > 64, where a chunk's few rows on a sequence far
+ * longer than the others take as long as that sequence alone), or -1. */
 int64_t m2c_kv_attend_chunk_workspace(const m2c_kv_cache* cache, int32_t n, int64_t total,
                                       int32_t n_heads, int32_t max_q, int32_t max_len);
 
@@ -703,7 +704,8 @@ int64_t m2c_kv_attend_chunk_workspace(const m2c_kv_cache* cache, int32_t n, int6
  * A sequence id out of range is reported, its rows become zeros (lse -infinity);
  * row starts that do not ascend are reported and touch nothing out of range.
  * bf16 caches: blocks of values whose scale is below 2^-80 of another's, or of the
- * 16-bit values', may count as larger, up to that. Results are the same bits on every run with the same arguments. */
+ * 16-bit values', may count as larger, up to that; values near the type's largest,
+ * whose sum over a row's keys times 2^14 leaves fp32, may give infinities. Results are the same bits on every run with the same arguments. */
 m2c_status m2c_kv_attend_chunk(const m2c_kv_cache* cache, const int32_t* seqs, int32_t n,
                                const int32_t* cu, int64_t total, int32_t n_heads, float scale,
                                const void* q, const int64_t q_stride[2], const void* k,
@@ -742,8 +744,8 @@ m2c_status m2c_kv_status(const m2c_kv_cache* cache, void* stream);
  *     out = N(r) weight + bias                                  (the next block's input)
  *     N(z) = (z - mean z) / sqrt(mean (z - mean z)^2 + eps), mean z taken as 0
  *            for M2C_NORM_RMS
- * All of it in fp32 (sums that leave its range in 64 bits), each output rounded
- * once: out is of r, not of what x_out's type keeps of it. */
+ * All of it in fp32 (sums that leave its range in 64 bits, the row brought near 1 by
+ * a power of two then), each output rounded once: out is of r, not of what x_out's type keeps of it. */
 enum { M2C_NORM_RMS = 0, M2C_NORM_LAYER = 1 };
 
 typedef struct {

@@ -7,7 +7,9 @@
 // dependent loads (length, tail, table) and the arrivals at the length. With keys
 // turned on their way and queries by further workgroups of the same launch: 8 tokens
 // for 32 heads of each 8.9 us; 40000 tokens of 64 query and 8 key heads of 128, 1.56
-// GB in 309 to 327 us (4.8 to 5.0 TB/s).
+// GB in 309 to 327 us (4.8 to 5.0 TB/s), with the turned keys in rows as well 1.64 GB
+// in 326; 3000 of 40 and 40 heads 36.4 us and with them 37.8 (rotation and append one
+// after the other: 344 and 42.3).
 #include <algorithm>
 
 #include "kv_device.h"

@@ -3,10 +3,15 @@
 //   N(z) = (z - mean z) / sqrt(mean (z - mean z)^2 + eps)   (mean 0 for M2C_NORM_RMS).
 // A row is read once and kept in registers, 8 consecutive elements of it per
 // thread and step, between the sums (one for each mean, over the wave by lane
-// exchanges and over the waves of a row through LDS) and what is written. Bound by
-// memory: 10692 rows of 8192, x and what comes of it in fp32, y and N in bf16, are
+// exchanges and over the waves of a row through LDS) and what is written; of rows
+// of more than 32768 elements, 64 a thread, most of that is in scratch memory (350
+// to 500 spilled registers). Bound by memory: 10692 rows of 8192, x and what comes of it in fp32, y and N in bf16, are
 // 1.05 GB in 185 us from a graph and 200 to 215 between other kernels (5.7 and 4.9
 // to 5.3 TB/s; a 1 GiB copy: 5.1). One row: 2.4 us, the two sums one after another.
+// x fp32, y fp16: 8000 rows of 5000 86 us, of 5001 or at odd addresses 124 to 130:
+// types known at run time only stand as branches between the loads, and take 110
+// registers for 70, so a CU holds one row of ten waves, not two. y bf16: 1000 rows of
+// 32768 88 us (4.5 TB/s), of 40000 119, of 65536 200 (3.9 TB/s), 65535 270.
 #include <type_traits>
 
 #include "attn_device.h"
@@ -270,8 +275,9 @@ hipError_t launch_rows(const NormArgs& A, hipStream_t stream) {
 
 // As few elements to a thread as a workgroup of 1024 threads allows. 20000 rows of
 // 1024: 37.0 us with 8 a thread, 38.5 with 16; 8192 of 4096: 72 and 76; 10692 of
-// 8192: 185, 187 and 196 with 32; 889 of 5120: 12.1, 12.4 and 11.4. Four rows of
-// one wave each to a workgroup took as long as one.
+// 8192: 185, 187 and 196 with 32. Rows that come to little more than run at once may
+// gain the other way: 889 of 5120, 1.7 times the 512 that do with 8 a thread, 12.1,
+// 12.4 and 11.4. Four rows of one wave each to a workgroup took as long as one.
 template <bool BF, bool X32, bool Y32, bool O32, bool VEC>
 hipError_t launch_typed(const NormArgs& A, hipStream_t stream) {
   if (A.d <= 8192) return launch_rows<BF, X32, Y32, O32, 1, VEC>(A, stream);
