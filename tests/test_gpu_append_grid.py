@@ -30,22 +30,21 @@ def test_more_blocks_than_a_grid_has_threads(turned, tokens):
     at = torch.arange(tokens, dtype=torch.int32, device="cuda")
     rotary = Rotary(torch.tensor([1e4 ** (-i / 32) for i in range(32)], dtype=torch.float32, device="cuda"))
     c, want = KVCache(2, HEADS, D, 2, BLOCK), KVCache(1, HEADS, D, 2, BLOCK)
-    end = slice(tokens - LAST, tokens)
+    end, place = slice(tokens - LAST, tokens), torch.tensor([0, LAST], dtype=torch.int32, device="cuda")
     if turned:
         q = rand((tokens, 3, D), 3)
         got, _ = c.append_rotated(rotary, k, v, at, q=q, cu=cu)
         for part in (slice(0, 5000), slice(tokens // 2, tokens // 2 + 5000), slice(tokens - 5000, tokens)):
             assert torch.equal(got[part], rotary.rotate(q[part], at[part]))
-        want.append_rotated(rotary, k[end], v[end], at[end], cu=cu[:2] * 0 + torch.tensor([0, LAST], dtype=torch.int32, device="cuda"))
+        want.append_rotated(rotary, k[end], v[end], at[end], cu=place)
     else:
         c.append(k, v, cu=cu)
-        want.append(k[end], v[end], cu=torch.tensor([0, LAST], dtype=torch.int32, device="cuda"))
+        want.append(k[end], v[end], cu=place)
     want.check()
     with pytest.raises(m2c.M2CError) as e:
         c.check()
     assert e.value.status == m2c.M2C_ERR_CAPACITY  # the first sequence, which stays as it was
     assert c.len.tolist() == [0, LAST] and want.len.tolist() == [LAST]
-    place = torch.tensor([0, LAST], dtype=torch.int32, device="cuda")
     got = c.read(place, LAST, seqs=torch.tensor([1], dtype=torch.int32, device="cuda"))
     for a, b in zip(got, want.read(place, LAST)):
         assert torch.equal(a, b)
